@@ -241,7 +241,7 @@ def _own_quantize(api, s):
 
 def _own_pointwise(api, s):
     codes, scales = api.ssconv_quantize_mxfp4(s["x"])
-    return api.ssconv_forward_dense_mxfp4(s["desc"], codes, scales, s["w_codes"], s["w_scales"], s["bias"])
+    return api.ssconv_forward_dense_mxfp4(s["desc"], codes, scales, s["w_codes"], s["w_scales"], s["bias"]).view(s["case"]["rows"], -1)
 
 
 def _plain_norm(case, grads):
