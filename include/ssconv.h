@@ -486,6 +486,90 @@ int32_t ssconv_forward_fp8(const ssconv_desc_t* desc, const void* x_e4m3, const 
 int32_t ssconv_forward_dense_fp8(const ssconv_desc_t* desc, const void* x_e4m3, const void* w_e4m3, const float* bias,
                                  float out_scale, void* y, int32_t* dev_status, void* stream);
 
+/* ---- The end of a training step over all tensors of a network -----------------------------------
+ * A mask-learning step ends with one update of the choice weights of every layer (Appendix, training details); these calls take
+ * all layers' tensors at once.  Tensors are given by HOST arrays of device pointers and element counts, read before the call
+ * returns; `type` (nullable: all SSCONV_F32) holds SSCONV_F32 or SSCONV_BF16 per tensor.  Pointers need the alignment of their
+ * elements (16-byte ones are read faster); n[i] = 0 is allowed, its pointer is then ignored.  SSCONV_ERR_BAD_DESC: a negative
+ * count, an unknown type, written tensors that overlap other tensors of the call (the same one twice, say; out[i] == g[i] is
+ * allowed). SSCONV_ERR_UNSUPPORTED_SHAPE: more than 2^40 elements.  No counterpart in the paper: it updates one layer's weights
+ * at a time and does not clip.
+ *
+ * ssconv_grad_norm:  norm[0] = sqrt(sum of all squares) (SSCONV_GRAD_NORM_L2) or the largest magnitude (SSCONV_GRAD_NORM_INF); 0
+ *   without elements.  Sums are held in 64 bits and taken in an order that depends on the counts alone, so that results are
+ *   reproducible; no finite gradients overflow on the way.  A NaN among the gradients makes the norm NaN (an infinity makes it
+ *   infinite).  norm: device fp32 [1]; ws: device scratch of ssconv_grad_norm_ws_bytes(tensors) bytes, 8-byte aligned, that no
+ *   other call in flight uses.
+ * ssconv_clip_grads:  out[i] = g[i] * min(1, max_norm / (norm + 1e-6)), in the type of g[i], rounded once; norm as written by
+ *   ssconv_grad_norm.  A NaN norm makes all gradients NaN, an infinite one makes the finite ones 0.
+ * ssconv_adamw_multi:  ssconv_adamw's update of every tensor with g[i] scaled as by ssconv_clip_grads (norm = NULL: not scaled);
+ *   theta, m, v: fp32; `type` is that of g.  The hyperparameters are doubles: 1 - beta is taken before rounding to fp32. */
+enum { SSCONV_F32 = 0, SSCONV_BF16 = 1 };
+enum { SSCONV_GRAD_NORM_L2 = 0, SSCONV_GRAD_NORM_INF = 1 };
+int32_t ssconv_grad_norm_ws_bytes(int32_t tensors, size_t* bytes);
+int32_t ssconv_grad_norm(const void* const* g, const int64_t* n, const int32_t* type, int32_t tensors, int32_t kind, float* norm,
+                         void* ws, size_t ws_bytes, void* stream);
+int32_t ssconv_clip_grads(const void* const* g, void* const* out, const int64_t* n, const int32_t* type, int32_t tensors,
+                          const float* norm, float max_norm, void* stream);
+int32_t ssconv_adamw_multi(void* const* theta, const void* const* g, void* const* m, void* const* v, const int64_t* n,
+                           const int32_t* type, int32_t tensors, int32_t step, double lr, double beta1, double beta2, double eps,
+                           double weight_decay, const float* norm, float max_norm, void* stream);
+
+/* ---- The end of a block and the beginning of the next one ----------------------------------------
+ * The norm of a block's output, its gate, the scaled residual and the next block's norm in one pass over rows of C channels (a row
+ * is a pixel); the layer scale, skip connection and norms of the ConvNeXt blocks of Sec. 4 are of this kind.  No counterpart in
+ * the paper's method.
+ *   p = post(b),   h = scale * x + gate .* p,   y = pre(h),
+ * post and pre: SSCONV_NORM_NONE (p = b; no y), SSCONV_NORM_LAYER ((v - mean) / sqrt(var + eps) * gamma + beta, biased variance)
+ * or SSCONV_NORM_RMS (v / sqrt(mean(v^2) + eps) * gamma + beta).  gamma, beta: fp32 [C], NULL for ones and zeros.  gate: fp32,
+ * NULL (ones), [C] with rows_per_gate = 0, or [ceil(rows / rows_per_gate)][C]: row r takes gates r / rows_per_gate.  x, b, h, y: bf16
+ * [rows][C]; arithmetic in fp32, y is the norm of h before h is rounded.  stats (nullable): fp32 [rows][4], what the backward call
+ * needs of both norms (mean and 1/deviation of b, then of h).  h (nullable if y is wanted) and y may be the buffer of x or of b.
+ * C % 8 == 0, C <= 8192, rows <= 2^30 (rows = 0 is a no-op); tensors 16-byte aligned. */
+enum { SSCONV_NORM_NONE = 0, SSCONV_NORM_LAYER = 1, SSCONV_NORM_RMS = 2 };
+typedef struct {
+  int64_t rows, rows_per_gate;
+  int32_t C, post, pre;
+  float scale, eps;
+} ssconv_resnorm_t;
+int32_t ssconv_residual_norm(const ssconv_resnorm_t* desc, const void* x, const void* b, const float* gate,
+                             const float* post_gamma, const float* post_beta, const float* pre_gamma, const float* pre_beta,
+                             void* h, void* y, float* stats, void* stream);
+/* Its gradients, from dh = dL/dh (nullable: zero) and dy = dL/dy (required with a second norm, ignored without): dx, db bf16
+ * [rows][C]; dgate of the shape of gate; dpost_gamma, dpost_beta, dpre_gamma, dpre_beta fp32 [C]: sums over rows in fp32, in a fixed
+ * order.  Any output may be NULL (not computed); those of a norm that is not there must be.  stats: as the forward call wrote them
+ * (ignored without norms).  rows = 0 writes zeros to dgate (if shared) and to the gradients of the norms' parameters.  ws: device
+ * scratch of ssconv_residual_norm_ws_bytes bytes, 16-byte aligned, that no other call in flight uses.  Outputs must not overlap
+ * inputs. */
+int32_t ssconv_residual_norm_ws_bytes(const ssconv_resnorm_t* desc, size_t* bytes);
+int32_t ssconv_residual_norm_backward(const ssconv_resnorm_t* desc, const void* x, const void* b, const float* stats,
+                                      const void* dh, const void* dy, const float* gate, const float* post_gamma,
+                                      const float* post_beta, const float* pre_gamma, void* dx, void* db, float* dgate,
+                                      float* dpost_gamma, float* dpost_beta, float* dpre_gamma, float* dpre_beta, void* ws,
+                                      size_t ws_bytes, void* stream);
+
+/* ---- 4-bit operands with a scale per block (MXFP4) -----------------------------------------------
+ * Rows of C channels in blocks of 32 (the last one of a row may be shorter): a block holds the scale 2^(floor(log2(largest
+ * magnitude)) - 2), at least 2^-127, as an 8-bit exponent, and per channel the nearest of 0, .5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives to x / scale (e2m1; ties to the even code; above 6: 6).  A block with an infinity or a NaN becomes NaN as a whole (scale
+ * code 255).  The paper's masks are stated for any operand type (Sec. 2, Sec. 3.1); the 2:4 form of the 4-bit tensor-core
+ * operation wants its kept values in neighbouring pairs, which these patterns are not, so 4-bit layers are dense (masked weights
+ * go in with their zeros).
+ *   codes:  [rows][ceil(C/32) * 16] bytes, two channels per byte, the lower one in the low half, zeros past C.
+ *   scales: bytes in the tile order of the tensor-core instruction, padded to whole tiles; every byte of both is written.
+ * ssconv_sizes_mxfp4 gives the sizes of both.  x: bf16 [rows][C], 16-byte aligned; C % 8 == 0; rows >= 0. */
+int32_t ssconv_sizes_mxfp4(int64_t rows, int32_t C, size_t* code_bytes, size_t* scale_bytes);
+int32_t ssconv_quantize_mxfp4(const void* x_bf16, int64_t rows, int32_t C, void* codes, void* scales, void* stream);
+/* The values the codes stand for (exact in bf16). */
+int32_t ssconv_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int32_t C, void* x_bf16, void* stream);
+/* Point-wise layer (KH = KW = 1, unit stride, no padding; anything else is SSCONV_ERR_UNSUPPORTED_SHAPE) on quantised operands:
+ *   y = act( bias + sum over ci of x_q[p, ci] * w_q[co, ci] ),
+ * x: the N*H*W pixels as rows of C_in channels, w: the C_out rows of the weights, both as ssconv_quantize_mxfp4 writes them; products
+ * and scales on the block-scaled tensor-core instruction, fp32 accumulation, one rounding to bf16.  C_in % 8 == 0, C_out % 8 == 0;
+ * flags as for ssconv_forward; pointers 16-byte aligned. */
+int32_t ssconv_forward_dense_mxfp4(const ssconv_desc_t* desc, const void* x_codes, const void* x_scales, const void* w_codes,
+                                   const void* w_scales, const float* bias, void* y, int32_t* dev_status, void* stream);
+
 /* Folding of f neighbouring output pixels of a row into the output channels.  A tile of the forward
  * kernels always spends 128 accumulator rows on output channels, so a layer with C_out <= 64 wastes
  * half of every multiply-add it issues.  The convolution of Eq. 4 with KW taps of stride s and

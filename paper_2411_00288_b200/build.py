@@ -10,8 +10,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libssconv.so")
-SOURCES = ["api.cu", "mask.cu", "pool.cu", "depthwise.cu", "train.cu", "wgrad.cu", "forward.cu"]
-HEADERS = ["launch.cuh", "layout.cuh", "sm100_ptx.cuh"]
+SOURCES = ["api.cu", "mask.cu", "pool.cu", "depthwise.cu", "train.cu", "wgrad.cu", "forward.cu",
+           "optim.cu", "resnorm.cu", "mxfp4.cu"]
+HEADERS = ["launch.cuh", "layout.cuh", "sm100_ptx.cuh", "activation.cuh", "optim.cuh", "resnorm.cuh", "mxfp4.cuh"]
 
 
 def _newest_source_mtime() -> float:

@@ -2,7 +2,14 @@
 // touches device memory, synchronises or allocates.
 #include <cuda_runtime.h>
 
+#include <algorithm>
+#include <new>
+#include <vector>
+
 #include "layout.cuh"
+#include "mxfp4.cuh"
+#include "optim.cuh"
+#include "resnorm.cuh"
 #include "ssconv.h"
 
 namespace ssconv {
@@ -136,6 +143,72 @@ int32_t check_depthwise(const ssconv_desc_t* desc, const void* x, const void* w_
   if (!aligned16(x) || !aligned16(w_bf16) || !aligned16(y)) return SSCONV_ERR_ALIGNMENT;
   if (desc->stride_h != desc->stride_w || desc->pad_h != desc->pad_w || desc->dil_h != desc->dil_w)
     return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  return SSCONV_OK;
+}
+
+// A call's tensors over many arrays: counts, types, pointers and the alignment of their elements.
+constexpr int64_t kMostElements = 1ll << 40;
+int32_t check_list(const void* const* p, const int64_t* n, const int32_t* type, int32_t tensors) {
+  for (int32_t i = 0; i < tensors; ++i) {
+    if (n[i] == 0) continue;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p[i]);
+    if (a == 0) return SSCONV_ERR_NULL;
+    if (a & (type != nullptr && type[i] == SSCONV_BF16 ? 1u : 3u)) return SSCONV_ERR_ALIGNMENT;
+  }
+  return SSCONV_OK;
+}
+int32_t check_counts(const int64_t* n, const int32_t* type, int32_t tensors) {
+  if (tensors < 0) return SSCONV_ERR_BAD_DESC;
+  if (tensors > 0 && !n) return SSCONV_ERR_NULL;
+  int64_t total = 0;
+  for (int32_t i = 0; i < tensors; ++i) {
+    if (n[i] < 0 || (type != nullptr && type[i] != SSCONV_F32 && type[i] != SSCONV_BF16)) return SSCONV_ERR_BAD_DESC;
+    if (n[i] > kMostElements || (total += n[i]) > kMostElements) return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  }
+  return SSCONV_OK;
+}
+
+// Memory that a call reads or writes, to see that nothing it writes is touched twice: two threads would then do it at the
+// same time.
+struct Span {
+  uintptr_t begin, end;
+  bool written;
+};
+void add_spans(std::vector<Span>& spans, const void* const* p, const int64_t* n, const int32_t* type, int32_t tensors, bool written,
+               const void* const* same = nullptr) {
+  for (int32_t i = 0; i < tensors; ++i) {
+    if (n[i] == 0 || (same != nullptr && same[i] == p[i])) continue;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p[i]);
+    spans.push_back({a, a + (uintptr_t)n[i] * (type != nullptr && type[i] == SSCONV_BF16 ? 2 : 4), written});
+  }
+}
+bool written_once(std::vector<Span>& spans) {
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  uintptr_t read = 0, written = 0;  // furthest ends so far
+  for (const Span& s : spans) {
+    if (s.begin < written || (s.written && s.begin < read)) return false;
+    uintptr_t& last = s.written ? written : read;
+    last = std::max(last, s.end);
+  }
+  return true;
+}
+
+int32_t check_resnorm(const ssconv_resnorm_t* d) {
+  if (!d) return SSCONV_ERR_NULL;
+  if (d->rows < 0 || d->rows_per_gate < 0 || d->C <= 0 || !(d->eps >= 0.0f) || !std::isfinite(d->eps) || !std::isfinite(d->scale))
+    return SSCONV_ERR_BAD_DESC;
+  for (const int32_t kind : {d->post, d->pre})
+    if (kind != SSCONV_NORM_NONE && kind != SSCONV_NORM_LAYER && kind != SSCONV_NORM_RMS) return SSCONV_ERR_BAD_DESC;
+  if (d->C % 8 != 0 || d->C > ssconv::kResnormMostC || d->rows > (1ll << 30)) return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  return SSCONV_OK;
+}
+
+int32_t check_mxfp4(int64_t rows, int32_t C) {
+  if (rows < 0 || C <= 0) return SSCONV_ERR_BAD_DESC;
+  if (C % 8 != 0 || rows > 0x7FFFFF00LL) return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  const ssconv::MxGeometry g = ssconv::mx_geometry(rows, C);
+  // (row, chunk of 128 channels) pairs and pieces of 8 channels are numbered in 32 bits, blocks of 256 pieces in 31
+  if (g.row_tiles * 128 * g.chunks > 0xFFFFFF00LL) return SSCONV_ERR_UNSUPPORTED_SHAPE;
   return SSCONV_OK;
 }
 
@@ -1009,6 +1082,178 @@ int32_t ssconv_forward_static_ws(const ssconv_desc_t* desc, const void* x, const
   if ((desc->flags & SSCONV_FLAG_BIAS) && !bias) return SSCONV_ERR_NULL;
   if (!aligned16(x) || !aligned16(w_comp) || !aligned16(meta) || !aligned16(y)) return SSCONV_ERR_ALIGNMENT;
   return ssconv::launch_forward_static_ws(*desc, x, w_comp, meta, bias, y, dev_status, (cudaStream_t)stream);
+}
+
+int32_t ssconv_grad_norm_ws_bytes(int32_t tensors, size_t* bytes) {
+  if (!bytes) return SSCONV_ERR_NULL;
+  if (tensors < 0) return SSCONV_ERR_BAD_DESC;
+  *bytes = ssconv::grad_norm_scratch(tensors);
+  return SSCONV_OK;
+}
+
+int32_t ssconv_grad_norm(const void* const* g, const int64_t* n, const int32_t* type, int32_t tensors, int32_t kind, float* norm, void* ws,
+                         size_t ws_bytes, void* stream) {
+  if (kind != SSCONV_GRAD_NORM_L2 && kind != SSCONV_GRAD_NORM_INF) return SSCONV_ERR_BAD_DESC;
+  int32_t rc = check_counts(n, type, tensors);
+  if (rc != SSCONV_OK) return rc;
+  if ((tensors > 0 && !g) || !norm) return SSCONV_ERR_NULL;
+  rc = check_list(g, n, type, tensors);
+  if (rc != SSCONV_OK) return rc;
+  if ((reinterpret_cast<uintptr_t>(norm) & 3u) || (reinterpret_cast<uintptr_t>(ws) & 7u)) return SSCONV_ERR_ALIGNMENT;
+  if (!ws || ws_bytes < ssconv::grad_norm_scratch(tensors)) return SSCONV_ERR_WORKSPACE;
+  return ssconv::launch_grad_norm(g, n, type, tensors, kind == SSCONV_GRAD_NORM_INF, norm, static_cast<double*>(ws), (cudaStream_t)stream) ==
+                 cudaSuccess
+             ? SSCONV_OK
+             : SSCONV_ERR_CUDA;
+}
+
+int32_t ssconv_clip_grads(const void* const* g, void* const* out, const int64_t* n, const int32_t* type, int32_t tensors, const float* norm,
+                          float max_norm, void* stream) {
+  if (!(max_norm >= 0.0f)) return SSCONV_ERR_BAD_DESC;
+  int32_t rc = check_counts(n, type, tensors);
+  if (rc != SSCONV_OK) return rc;
+  if (tensors == 0) return SSCONV_OK;
+  if (!g || !out || !norm) return SSCONV_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(norm) & 3u) return SSCONV_ERR_ALIGNMENT;
+  for (const void* const* list : {g, const_cast<const void* const*>(out)}) {
+    rc = check_list(list, n, type, tensors);
+    if (rc != SSCONV_OK) return rc;
+  }
+  try {
+    std::vector<Span> spans;
+    spans.reserve(2 * (size_t)tensors);
+    add_spans(spans, out, n, type, tensors, true);
+    add_spans(spans, g, n, type, tensors, false, out);
+    if (!written_once(spans)) return SSCONV_ERR_BAD_DESC;
+  } catch (const std::bad_alloc&) {
+    return SSCONV_ERR_CUDA;
+  }
+  return ssconv::launch_clip_grads(g, out, n, type, tensors, norm, max_norm, (cudaStream_t)stream) == cudaSuccess ? SSCONV_OK : SSCONV_ERR_CUDA;
+}
+
+int32_t ssconv_adamw_multi(void* const* theta, const void* const* g, void* const* m, void* const* v, const int64_t* n, const int32_t* type,
+                           int32_t tensors, int32_t step, double lr, double beta1, double beta2, double eps, double weight_decay,
+                           const float* norm, float max_norm, void* stream) {
+  if (step < 1 || !(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || (norm && !(max_norm >= 0.0f)))
+    return SSCONV_ERR_BAD_DESC;
+  int32_t rc = check_counts(n, type, tensors);
+  if (rc != SSCONV_OK) return rc;
+  if (tensors == 0) return SSCONV_OK;
+  if (!theta || !g || !m || !v) return SSCONV_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(norm) & 3u) return SSCONV_ERR_ALIGNMENT;
+  rc = check_list(g, n, type, tensors);
+  if (rc != SSCONV_OK) return rc;
+  for (void* const* list : {theta, m, v}) {
+    rc = check_list(const_cast<const void* const*>(list), n, nullptr, tensors);
+    if (rc != SSCONV_OK) return rc;
+  }
+  try {
+    std::vector<Span> spans;
+    spans.reserve(4 * (size_t)tensors);
+    for (void* const* list : {theta, m, v}) add_spans(spans, const_cast<const void* const*>(list), n, nullptr, tensors, true);
+    add_spans(spans, g, n, type, tensors, false);
+    if (!written_once(spans)) return SSCONV_ERR_BAD_DESC;
+  } catch (const std::bad_alloc&) {
+    return SSCONV_ERR_CUDA;
+  }
+  const ssconv::AdamwParams a = {(float)lr, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
+                                 (float)weight_decay, (float)(1.0 / (1.0 - std::pow(beta1, (double)step))),
+                                 (float)(1.0 / (1.0 - std::pow(beta2, (double)step)))};
+  return ssconv::launch_adamw_multi(theta, g, m, v, n, type, tensors, a, norm, max_norm, (cudaStream_t)stream) == cudaSuccess ? SSCONV_OK
+                                                                                                                             : SSCONV_ERR_CUDA;
+}
+
+int32_t ssconv_residual_norm(const ssconv_resnorm_t* desc, const void* x, const void* b, const float* gate, const float* post_gamma,
+                             const float* post_beta, const float* pre_gamma, const float* pre_beta, void* h, void* y, float* stats,
+                             void* stream) {
+  const int32_t rc = check_resnorm(desc);
+  if (rc != SSCONV_OK) return rc;
+  if (desc->rows == 0) return SSCONV_OK;
+  if (!x || !b || (!h && !y) || (desc->pre != SSCONV_NORM_NONE && !y)) return SSCONV_ERR_NULL;
+  if (desc->pre == SSCONV_NORM_NONE && y) return SSCONV_ERR_BAD_DESC;
+  if (h && h == y) return SSCONV_ERR_BAD_DESC;
+  for (const void* p : {x, b, (const void*)gate, (const void*)post_gamma, (const void*)post_beta, (const void*)pre_gamma, (const void*)pre_beta,
+                        (const void*)h, (const void*)y, (const void*)stats})
+    if (!aligned16(p)) return SSCONV_ERR_ALIGNMENT;
+  return ssconv::launch_resnorm(*desc, {x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, h, y, stats}, (cudaStream_t)stream) == cudaSuccess
+             ? SSCONV_OK
+             : SSCONV_ERR_CUDA;
+}
+
+int32_t ssconv_residual_norm_ws_bytes(const ssconv_resnorm_t* desc, size_t* bytes) {
+  if (!bytes) return SSCONV_ERR_NULL;
+  const int32_t rc = check_resnorm(desc);
+  if (rc != SSCONV_OK) return rc;
+  *bytes = ssconv::resnorm_scratch(*desc);
+  return SSCONV_OK;
+}
+
+int32_t ssconv_residual_norm_backward(const ssconv_resnorm_t* desc, const void* x, const void* b, const float* stats, const void* dh,
+                                      const void* dy, const float* gate, const float* post_gamma, const float* post_beta,
+                                      const float* pre_gamma, void* dx, void* db, float* dgate, float* dpost_gamma, float* dpost_beta,
+                                      float* dpre_gamma, float* dpre_beta, void* ws, size_t ws_bytes, void* stream) {
+  const int32_t rc = check_resnorm(desc);
+  if (rc != SSCONV_OK) return rc;
+  const bool post = desc->post != SSCONV_NORM_NONE, pre = desc->pre != SSCONV_NORM_NONE;
+  if ((!post && (dpost_gamma || dpost_beta)) || (!pre && (dpre_gamma || dpre_beta))) return SSCONV_ERR_BAD_DESC;
+  for (const void* p : {x, b, (const void*)stats, dh, dy, (const void*)gate, (const void*)post_gamma, (const void*)post_beta,
+                        (const void*)pre_gamma, (const void*)dx, (const void*)db, (const void*)dgate, (const void*)dpost_gamma,
+                        (const void*)dpost_beta, (const void*)dpre_gamma, (const void*)dpre_beta, (const void*)ws})
+    if (!aligned16(p)) return SSCONV_ERR_ALIGNMENT;
+  if (desc->rows == 0) {
+    for (float* sum : {desc->rows_per_gate == 0 ? dgate : nullptr, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta})
+      if (sum && cudaMemsetAsync(sum, 0, sizeof(float) * desc->C, (cudaStream_t)stream) != cudaSuccess) return SSCONV_ERR_CUDA;
+    return SSCONV_OK;
+  }
+  if (!x || !b || ((post || pre) && !stats) || (pre && !dy) || (!pre && !dh)) return SSCONV_ERR_NULL;
+  if (!ws || ws_bytes < ssconv::resnorm_scratch(*desc)) return SSCONV_ERR_WORKSPACE;
+  return ssconv::launch_resnorm_backward(*desc, {x, b, gate, post_gamma, post_beta, pre_gamma, nullptr, nullptr, nullptr, const_cast<float*>(stats)},
+                                         {dh, dy, dx, db, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta}, static_cast<float*>(ws),
+                                         (cudaStream_t)stream) == cudaSuccess
+             ? SSCONV_OK
+             : SSCONV_ERR_CUDA;
+}
+
+int32_t ssconv_sizes_mxfp4(int64_t rows, int32_t C, size_t* code_bytes, size_t* scale_bytes) {
+  const int32_t rc = check_mxfp4(rows, C);
+  if (rc != SSCONV_OK) return rc;
+  const ssconv::MxGeometry g = ssconv::mx_geometry(rows, C);
+  if (code_bytes) *code_bytes = (size_t)rows * g.blocks * 16;
+  if (scale_bytes) *scale_bytes = (size_t)g.row_tiles * g.chunks * ssconv::kMxImageBytes;
+  return SSCONV_OK;
+}
+
+int32_t ssconv_quantize_mxfp4(const void* x_bf16, int64_t rows, int32_t C, void* codes, void* scales, void* stream) {
+  const int32_t rc = check_mxfp4(rows, C);
+  if (rc != SSCONV_OK) return rc;
+  if (rows == 0) return SSCONV_OK;
+  if (!x_bf16 || !codes || !scales) return SSCONV_ERR_NULL;
+  if (!aligned16(x_bf16) || !aligned16(codes) || !aligned16(scales)) return SSCONV_ERR_ALIGNMENT;
+  return ssconv::launch_quantize_mxfp4(x_bf16, rows, C, codes, scales, (cudaStream_t)stream) == cudaSuccess ? SSCONV_OK : SSCONV_ERR_CUDA;
+}
+
+int32_t ssconv_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int32_t C, void* x_bf16, void* stream) {
+  const int32_t rc = check_mxfp4(rows, C);
+  if (rc != SSCONV_OK) return rc;
+  if (rows == 0) return SSCONV_OK;
+  if (!x_bf16 || !codes || !scales) return SSCONV_ERR_NULL;
+  if (!aligned16(x_bf16) || !aligned16(codes) || !aligned16(scales)) return SSCONV_ERR_ALIGNMENT;
+  return ssconv::launch_dequantize_mxfp4(codes, scales, rows, C, x_bf16, (cudaStream_t)stream) == cudaSuccess ? SSCONV_OK : SSCONV_ERR_CUDA;
+}
+
+int32_t ssconv_forward_dense_mxfp4(const ssconv_desc_t* desc, const void* x_codes, const void* x_scales, const void* w_codes,
+                                   const void* w_scales, const float* bias, void* y, int32_t* dev_status, void* stream) {
+  int32_t rc = check_desc(desc, true);
+  if (rc != SSCONV_OK) return rc;
+  if (desc->KH != 1 || desc->KW != 1 || desc->stride_h != 1 || desc->stride_w != 1 || desc->pad_h != 0 || desc->pad_w != 0)
+    return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  rc = check_mxfp4((int64_t)desc->N * desc->H * desc->W, desc->C_in);
+  if (rc != SSCONV_OK) return rc;
+  if (!x_codes || !x_scales || !w_codes || !w_scales || !y) return SSCONV_ERR_NULL;
+  if ((desc->flags & SSCONV_FLAG_BIAS) && !bias) return SSCONV_ERR_NULL;
+  for (const void* p : {x_codes, x_scales, w_codes, w_scales, (const void*)bias, (const void*)y})
+    if (!aligned16(p)) return SSCONV_ERR_ALIGNMENT;
+  return ssconv::launch_forward_mxfp4(*desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,450 @@
+// Microscaled 4-bit operands: quantisation of bf16 rows, the way back, and the product of two such matrices (a point-wise layer)
+// on the block-scaled tensor-core instruction.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "activation.cuh"
+#include "launch.cuh"
+#include "layout.cuh"
+#include "mxfp4.cuh"
+#include "sm100_ptx.cuh"
+
+namespace ssconv {
+
+namespace {
+
+// ---------------------------------------------------------------------------------------
+// Quantisation.  The scale's exponent comes from the exponent field E of the block's largest magnitude: floor(log2) = E - 127, so
+// the code (bias 127) is E - 2, at least 0; E = 255 (an infinity or a NaN) gives 255.  Elements are multiplied by the inverse
+// power of two (exact) and rounded once.  Four lanes hold a block, 16 lanes a row's share of a scale image.  DRAM-bound:
+// 2.53 bytes per element.
+// ---------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, float scale) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t out;
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    f[2 * j] = bf16_lo(w[j]) * scale;
+    f[2 * j + 1] = bf16_hi(w[j]) * scale;
+  }
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(out)
+      : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
+  return out;
+}
+__device__ __forceinline__ uint32_t magnitude_bits(uint32_t pair) { return max(pair & 0x7FFFu, (pair >> 16) & 0x7FFFu); }
+
+__global__ void __launch_bounds__(256) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint32_t* scales, uint32_t rows, uint32_t items,
+                                                             uint32_t chunks, uint32_t blocks, uint32_t C8) {
+  grid_launch_dependents();
+  const uint32_t item = blockIdx.x * 16u + (threadIdx.x >> 4);  // (row, chunk)
+  const uint32_t lane = threadIdx.x & 15u;
+  const uint32_t row = item / chunks, chunk = item - row * chunks;
+  grid_dependency_wait();
+  if (item >= items) return;  // (whole halves of a warp: the shuffles below stay among 16 lanes)
+  const uint32_t mask = 0xFFFFu << (threadIdx.x & 16u);
+  const uint32_t piece = chunk * 16u + lane;  // of 8 channels
+  uint4 v = make_uint4(0u, 0u, 0u, 0u);
+  if (row < rows && piece < C8) v = x[(uint64_t)row * C8 + piece];
+  uint32_t m = max(max(magnitude_bits(v.x), magnitude_bits(v.y)), max(magnitude_bits(v.z), magnitude_bits(v.w)));
+  m = max(m, __shfl_xor_sync(mask, m, 1));
+  m = max(m, __shfl_xor_sync(mask, m, 2));
+  const uint32_t e = m >> 7;
+  const uint32_t code = e == 255u ? 255u : e < 2u ? 0u : e - 2u;
+  const float inverse = __uint_as_float((254u - min(code, 252u)) << 23);
+  if (row < rows && (piece >> 2) < blocks) codes[(uint64_t)row * (4u * blocks) + piece] = e2m1_x8(v, inverse);
+  uint32_t word = code << (8u * (lane >> 2));
+  word |= __shfl_xor_sync(mask, word, 4);
+  word |= __shfl_xor_sync(mask, word, 8);
+  if (lane == 0) scales[((uint64_t)(row >> 7) * chunks + chunk) * 128u + (row & 31u) * 4u + ((row >> 5) & 3u)] = word;
+}
+
+// The values of codes: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, times the scale; exact in bf16.
+__device__ __forceinline__ float e2m1_value(uint32_t code) {
+  const uint32_t e = (code >> 1) & 3u, m = code & 1u;
+  const uint32_t bits = e ? ((e + 126u) << 23) | (m << 22) : m * 0x3F000000u;
+  return __uint_as_float(bits | ((code & 8u) << 28));
+}
+__global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint64_t pieces, uint32_t C8,
+                                                               uint32_t chunks, uint32_t blocks) {
+  grid_launch_dependents();
+  const uint64_t i = blockIdx.x * (uint64_t)blockDim.x + threadIdx.x;
+  grid_dependency_wait();
+  if (i >= pieces) return;
+  const uint64_t row = i / C8;
+  const uint32_t piece = (uint32_t)(i - row * C8), block = piece >> 2;
+  const uint32_t s = scales[((row >> 7) * chunks + (block >> 2)) * 512u + (row & 31u) * 16u + ((row >> 5) & 3u) * 4u + (block & 3u)];
+  const float scale = __uint_as_float(s == 255u ? 0x7FC00000u : s == 0u ? 0x00400000u : s << 23);
+  const uint32_t c = codes[row * (4u * blocks) + piece];
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = e2m1_value(c >> (4 * j)) * scale;
+  x[i] = make_uint4(pack_bf16x2<false>(f[0], f[1]), pack_bf16x2<false>(f[2], f[3]), pack_bf16x2<false>(f[4], f[5]), pack_bf16x2<false>(f[6], f[7]));
+}
+
+// ---------------------------------------------------------------------------------------
+// Product.  y[p, co] = act(bias[co] + sum_ci x_q[p, ci] w_q[co, ci]): tiles of 128 pixels (the accumulator's rows) x BN channels,
+// K in stages of 256 channels (128 bytes of codes per row, the 128-byte swizzle; two scale images per 128 rows).  One thread block
+// per SM walks over tiles, channels first, so that the blocks at work at a time share few rows of x; two accumulators, so that a
+// tile's epilogue runs beside the next one's MMAs.  Warps 0-3 epilogue, 4 producer, 5 MMA issuer.
+// ---------------------------------------------------------------------------------------
+constexpr long long kMxWaitLimit = 4000000000LL;  // cycles: about 2 s
+constexpr int kMxThreads = 192;
+constexpr int kMxStoreBytes = 128 * 128;          // staged outputs: 128 pixels x 64 channels of bf16
+constexpr int kMxMostSmem = 227 * 1024;
+
+template <int BN>
+struct MxTile {
+  static constexpr int kScaleTiles = BN > 128 ? 2 : 1;  // images along the tile's channels
+  static constexpr int kBytesA = 128 * 128, kBytesB = BN * 128, kBytesScales = 1024 * (1 + kScaleTiles);
+  static constexpr int kBytes = kBytesA + kBytesB + kBytesScales;
+  static constexpr int kRoom = kMxMostSmem - 1024 - 2 * kMxStoreBytes - 256;
+  static constexpr int kStages = kRoom / kBytes < 6 ? kRoom / kBytes : 6;
+  static constexpr int kScaleColumns = 8 * (1 + kScaleTiles);  // of TMEM, per stage: two images of x, two (four) of w
+  static constexpr int kTmem = 2 * BN + kStages * kScaleColumns <= 256 ? 256 : 512;
+  static constexpr int kSmem = 1024 + kStages * kBytes + 2 * kMxStoreBytes + 256;
+  static_assert(2 * BN + kStages * kScaleColumns <= 512 && kStages >= 3, "");
+};
+
+struct MxParams {
+  const uint8_t *x_scales, *w_scales;
+  const float* bias;
+  int32_t* dev_status;
+  int m_tiles, n_tiles, w_tiles;  // w_tiles: scale images along C_out
+  int C_out, chunks, steps;       // steps of 64 channels
+};
+
+// 32x128b.warpx4: 512 bytes (32 rows of 16, unswizzled) into 4 TMEM columns, the same 32 lanes in each of the four quarters.
+__device__ __forceinline__ void tc_cp_32x128b_x4_w(uint32_t dst_tmem, uint32_t src_lo) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t.reg .b64 ds;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "mov.b64 ds, {%1, %2};\n\t"
+      "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], ds;\n\t}"
+      ::"r"(dst_tmem), "r"(src_lo), "r"(kDescHiNoSwizzle128)
+      : "memory");
+}
+// D[128 x N] (+)= A[128 x 64] B[N x 64]^T, e2m1 operands with one e8m0 scale per 32 elements of a row, taken from TMEM.
+__device__ __forceinline__ void tc_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                              uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "mov.b64 da, {%1, %7};\n\t"
+      "mov.b64 db, {%2, %7};\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(kDescHiSw128)
+      : "memory");
+}
+// Instruction descriptor of kind::mxf4: bits 4-5 and 29-30 which of a row's scales in its TMEM word (0 or 2: the first two or the
+// last two) for B and A, bits 7-9 and 10-12 the formats (1 = e2m1), bits 17-22 N >> 3, bit 23 the scales' format (1 = e8m0),
+// bits 27-28 M >> 7.
+__host__ __device__ constexpr uint32_t make_idesc_mxf4(uint32_t N, uint32_t which) {
+  return (which << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (1u << 23) | (1u << 27) | (which << 29);
+}
+// 32 columns of the warp's 32 lanes: register i of lane t holds column i of row t.
+__device__ __forceinline__ void tc_ld_32x32b_x32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+        "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void epilogue_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_group_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+
+template <int BN, int ACT>
+__global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
+                                                             const __grid_constant__ CUtensorMap tm_y, const MxParams p) {
+  using T = MxTile<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* ring_a = smem;
+  uint8_t* ring_b = ring_a + T::kStages * T::kBytesA;
+  uint8_t* staged = ring_b + T::kStages * T::kBytesB;
+  uint8_t* ring_s = staged + 2 * kMxStoreBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(ring_s + T::kStages * T::kBytesScales);
+  uint64_t *full = bars, *empty = bars + T::kStages, *acc_full = bars + 2 * T::kStages, *acc_empty = acc_full + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5;
+
+  grid_launch_dependents();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < T::kStages; ++s) {
+      mbar_init(full + s, 1);
+      mbar_init(empty + s, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(acc_full + i, 1);
+      mbar_init(acc_empty + i, 4);
+    }
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 4) {
+    prefetch_tensormap(&tm_x);
+    prefetch_tensormap(&tm_w);
+    prefetch_tensormap(&tm_y);
+  }
+  if (warp == 5) {
+    tmem_alloc(tmem_slot, T::kTmem);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  grid_dependency_wait();
+
+  const int tiles = p.m_tiles * p.n_tiles;
+  const int stages = (p.steps + 3) >> 2;
+  if (warp == 4) {
+    // ---------------------------------------------------------------- producer
+    const uint32_t a0 = smem_u32(ring_a), b0 = smem_u32(ring_b), s0 = smem_u32(ring_s), full0 = smem_u32(full), empty0 = smem_u32(empty);
+    uint32_t s = 0, phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+      const int m = t / p.n_tiles, n = t - m * p.n_tiles;
+      const uint8_t* xs = p.x_scales + (int64_t)m * p.chunks * kMxImageBytes;
+      const int first = n * BN >> 7;
+      const int images = min((n * BN + BN - 1) >> 7, p.w_tiles - 1) - first + 1;
+      for (int kb = 0; kb < stages; ++kb) {
+        if (!mbar_wait_warp_a(empty0 + 8 * s, phase ^ 1u, abort_flag, kMxWaitLimit)) {
+          ok = false;
+          break;
+        }
+        const uint32_t bar = full0 + 8 * s, sc = s0 + s * T::kBytesScales;
+        const uint32_t part = min(2, p.chunks - 2 * kb) * kMxImageBytes;
+        mbar_expect_tx_w(bar, T::kBytesA + T::kBytesB + part * (1 + images));
+        tma_load_2d_w(a0 + s * T::kBytesA, &tm_x, bar, kb * 128, m * 128);
+        tma_load_2d_w(b0 + s * T::kBytesB, &tm_w, bar, kb * 128, n * BN);
+        bulk_load_w(sc, xs + kb * 2 * kMxImageBytes, part, bar);
+        for (int i = 0; i < images; ++i)
+          bulk_load_w(sc + 1024 * (1 + i), p.w_scales + ((int64_t)(first + i) * p.chunks + 2 * kb) * kMxImageBytes, part, bar);
+        if (++s == T::kStages) {
+          s = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+  } else if (warp == 5) {
+    // ---------------------------------------------------------------- MMA issuer
+    const uint32_t a0 = desc_lo(smem_u32(ring_a)), b0 = desc_lo(smem_u32(ring_b)), s0 = desc_lo(smem_u32(ring_s));
+    const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
+    uint32_t s = 0, phase = 0, buf = 0, acc_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+      // tiles that start inside an image take its later columns
+      const uint32_t shift = ((uint32_t)(t % p.n_tiles) * BN & 127u) >> 5;
+      if (!mbar_wait_warp_a(acc_empty0 + 8 * buf, acc_phase ^ 1u, abort_flag, kMxWaitLimit)) break;
+      tc_fence_after();
+      const uint32_t d = tmem + buf * BN;
+      for (int kb = 0; kb < stages; ++kb) {
+        if (!mbar_wait_warp_a(full0 + 8 * s, phase, abort_flag, kMxWaitLimit)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t sfa = tmem + 2 * BN + s * T::kScaleColumns, sfb = sfa + 8;
+        const uint32_t src = s0 + s * (T::kBytesScales >> 4);
+        const int steps = min(4, p.steps - 4 * kb);
+        for (int c = 0; 2 * c < steps; ++c) {
+          tc_cp_32x128b_x4_w(sfa + 4 * c, src + 32 * c);
+#pragma unroll
+          for (int i = 0; i < T::kScaleTiles; ++i) tc_cp_32x128b_x4_w(sfb + 4 * T::kScaleTiles * c + 4 * i, src + 64 * (1 + i) + 32 * c);
+        }
+        for (int k = 0; k < steps; ++k)
+          tc_mma_mxf4_w(d, a0 + s * (T::kBytesA >> 4) + 2 * k, b0 + s * (T::kBytesB >> 4) + 2 * k, make_idesc_mxf4(BN, 2 * (k & 1)),
+                        sfa + 4 * (k >> 1), sfb + 4 * T::kScaleTiles * (k >> 1) + shift, (kb | k) != 0);
+        tc_commit_w(empty0 + 8 * s);
+        if (++s == T::kStages) {
+          s = 0;
+          phase ^= 1u;
+        }
+      }
+      if (!ok) break;
+      tc_commit_w(acc_full0 + 8 * buf);
+      buf ^= 1u;
+      if (buf == 0) acc_phase ^= 1u;
+    }
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    // (after a wait that ran out the warps go on through the barriers that they share, and touch nothing else)
+    const int row = threadIdx.x;
+    uint32_t buf = 0, acc_phase = 0, pieces = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+      const int m = t / p.n_tiles, n = t - m * p.n_tiles;
+      ok = mbar_wait_warp(acc_full + buf, acc_phase, abort_flag, kMxWaitLimit) && ok;
+      tc_fence_after();
+      const uint32_t acc = tmem + buf * BN + ((uint32_t)(warp * 32) << 16);
+#pragma unroll 1
+      for (int g = 0; g < BN / 64; ++g) {
+        const int c0 = n * BN + 64 * g;
+        if (c0 >= p.C_out) break;
+        if (threadIdx.x == 0) bulk_wait_group_read1();  // the buffer of the piece before the last one is free
+        epilogue_barrier();
+        uint8_t* out = staged + (pieces & 1) * kMxStoreBytes;
+        if (ok) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t r[32];
+            tc_ld_32x32b_x32(acc + 64 * g + 32 * half, r);
+            tc_wait_ld();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float v[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r[8 * q + j]);
+              const int c = c0 + 32 * half + 8 * q;
+              if (p.bias != nullptr && c < p.C_out) {
+                const float4 b0 = __ldg(reinterpret_cast<const float4*>(p.bias + c)), b1 = __ldg(reinterpret_cast<const float4*>(p.bias + c) + 1);
+                v[0] += b0.x; v[1] += b0.y; v[2] += b0.z; v[3] += b0.w;
+                v[4] += b1.x; v[5] += b1.y; v[6] += b1.z; v[7] += b1.w;
+              }
+              const uint4 o = make_uint4(activate_pack<ACT>(v[0], v[1]), activate_pack<ACT>(v[2], v[3]), activate_pack<ACT>(v[4], v[5]),
+                                         activate_pack<ACT>(v[6], v[7]));
+              *reinterpret_cast<uint4*>(out + row * 128 + (((4 * half + q) ^ (row & 7)) << 4)) = o;
+            }
+          }
+          fence_proxy_async_smem();
+        }
+        epilogue_barrier();
+        if (threadIdx.x == 0 && ok) {
+          tma_store_2d(&tm_y, out, c0, m * 128);
+          bulk_commit_group();
+        }
+        ++pieces;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if ((threadIdx.x & 31) == 0) mbar_arrive(acc_empty + buf);
+      buf ^= 1u;
+      if (buf == 0) acc_phase ^= 1u;
+    }
+    if (threadIdx.x == 0) bulk_wait_group_read0();
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag != 0) {
+    // give copies and MMAs still in flight time to land before shared memory and TMEM go away
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) __nanosleep(1000);
+    if (threadIdx.x == 0 && p.dev_status != nullptr) atomicExch(p.dev_status, (int)SSCONV_ERR_TIMEOUT);
+    __syncthreads();
+  }
+  if (warp == 5) {
+    tc_fence_after();
+    tmem_dealloc(tmem, T::kTmem);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encoder() {
+  static std::atomic<EncodeFn> known{nullptr};  // (every thread finds the same function)
+  EncodeFn f = known.load(std::memory_order_relaxed);
+  if (f == nullptr) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess || !p)
+      return nullptr;
+    f = reinterpret_cast<EncodeFn>(p);
+    known.store(f, std::memory_order_relaxed);
+  }
+  return f;
+}
+// A matrix of `rows` rows of `inner` elements, copied in boxes of 128 bytes x box_rows in the 128-byte swizzle.
+bool encode_matrix(EncodeFn f, CUtensorMap* map, CUtensorMapDataType type, int element, const void* base, int64_t inner, int64_t rows, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)inner * element};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / element), (cuuint32_t)box_rows}, ones[2] = {1, 1};
+  return f(map, type, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+using MxKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, MxParams);
+template <int BN>
+MxKernel mx_kernel(int act, int* smem) {
+  *smem = MxTile<BN>::kSmem;
+  return act == kActGelu ? mxfp4_kernel<BN, kActGelu> : act == kActRelu ? mxfp4_kernel<BN, kActRelu> : mxfp4_kernel<BN, kActNone>;
+}
+
+}  // namespace
+
+cudaError_t launch_quantize_mxfp4(const void* x, int64_t rows, int C, void* codes, void* scales, cudaStream_t st) {
+  const MxGeometry g = mx_geometry(rows, C);
+  const uint32_t items = (uint32_t)(g.row_tiles * 128 * g.chunks);
+  count_launch();
+  return launch_dependent(quantize_mxfp4_kernel, (items + 15u) / 16u, 256, st, (const uint4*)x, (uint32_t*)codes, (uint32_t*)scales, (uint32_t)rows,
+                          items, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
+}
+
+cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int C, void* x, cudaStream_t st) {
+  const MxGeometry g = mx_geometry(rows, C);
+  const uint64_t pieces = (uint64_t)rows * (C / 8);
+  count_launch();
+  return launch_dependent(dequantize_mxfp4_kernel, (unsigned)((pieces + 255) / 256), 256, st, (const uint32_t*)codes, (const uint8_t*)scales, (uint4*)x,
+                          pieces, (uint32_t)(C / 8), (uint32_t)g.chunks, (uint32_t)g.blocks);
+}
+
+int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales,
+                             const float* bias, void* y, int32_t* dev_status, cudaStream_t st) {
+  const int64_t rows = (int64_t)d.N * d.H * d.W;
+  const MxGeometry gx = mx_geometry(rows, d.C_in), gw = mx_geometry(d.C_out, d.C_in);
+  // The width that keeps the SMs busy: a tile costs its columns and a fixed part.
+  int dev = 0, major = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess)
+    return SSCONV_ERR_CUDA;
+  if (major != 10) return SSCONV_ERR_ARCH;
+  const int sms = device_sms();
+  int bn = 0;
+  int64_t least = 0;
+  for (const int w : {192, 128, 64}) {
+    const int64_t tiles = gx.row_tiles * ((d.C_out + w - 1) / w);
+    const int64_t cost = (tiles + sms - 1) / sms * (w + 32);
+    if (bn == 0 || cost < least) {
+      bn = w;
+      least = cost;
+    }
+  }
+  int smem = 0;
+  const int act = activation_of(d.flags);
+  const MxKernel kernel = bn == 192 ? mx_kernel<192>(act, &smem) : bn == 128 ? mx_kernel<128>(act, &smem) : mx_kernel<64>(act, &smem);
+  const EncodeFn encode = encoder();
+  if (encode == nullptr) return SSCONV_ERR_CUDA;
+  CUtensorMap tm_x, tm_w, tm_y;
+  const int64_t row_bytes = (int64_t)gx.blocks * 16;
+  if (!encode_matrix(encode, &tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x_codes, row_bytes, rows, 128) ||
+      !encode_matrix(encode, &tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, w_codes, row_bytes, d.C_out, bn) ||
+      !encode_matrix(encode, &tm_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, y, d.C_out, rows, 128))
+    return SSCONV_ERR_CUDA;
+  MxParams p = {static_cast<const uint8_t*>(x_scales), static_cast<const uint8_t*>(w_scales),
+                (d.flags & SSCONV_FLAG_BIAS) ? bias : nullptr, dev_status, (int)gx.row_tiles, (d.C_out + bn - 1) / bn, (int)gw.row_tiles,
+                d.C_out, gx.chunks, (gx.blocks + 1) / 2};
+  const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
+  if (tiles > 0x7FFFFFFF - 4096) return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SSCONV_ERR_CUDA;
+  count_launch();
+  return launch_dependent_smem(kernel, (unsigned)(tiles < sms ? tiles : sms), kMxThreads, smem, st, tm_x, tm_w, tm_y, p) == cudaSuccess
+             ? SSCONV_OK
+             : SSCONV_ERR_CUDA;
+}
+
+}  // namespace ssconv
