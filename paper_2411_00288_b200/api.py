@@ -848,32 +848,23 @@ def ssconv_dgrad_spread(desc: Desc, dy: torch.Tensor, stream=None) -> torch.Tens
     return out
 
 
-# ----------------------------------------------------------------------------- what the calls below ask of their tensors
-def _expect(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int) -> None:
-    """Refuse a tensor that is not `numel` contiguous elements of `dtype` on the current device."""
-    if t is None:
-        return
-    if t.dtype is not dtype:
-        raise TypeError(f"{name}: {dtype} is expected, not {t.dtype}")
-    if t.numel() != numel:
-        raise ValueError(f"{name}: {numel} elements are expected, not {t.numel()}")
-    if not (t.is_cuda and t.is_contiguous()) or t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: tensors must be contiguous and on the current CUDA device")
-
-
-def _new(stream, like: torch.Tensor, shape, dtype) -> torch.Tensor:
-    """An uninitialised tensor whose memory is free for the stream that the call runs on."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
-
-
 # ----------------------------------------------------------------------------- all tensors of a network
+# (These calls and the ones below check and allocate their tensors in the native binding, all for the current stream: another one
+# is made current around them.)
+def _on_stream(call):
+    """`call` with a keyword `stream`: a torch stream to run on, None for the current one."""
+    @functools.wraps(call)
+    def on(*args, stream=None, **kwargs):
+        if stream is None:
+            return call(*args, **kwargs)
+        with torch.cuda.stream(stream):
+            return call(*args, **kwargs)
+    return on
+
+
 GRAD_NORM_L2, GRAD_NORM_INF = 0, 1
 
 
-@functools.lru_cache(maxsize=1024)
 def ssconv_grad_norm_ws_bytes(tensors: int) -> int:
     """Scratch bytes of ssconv_grad_norm over that many tensors."""
     n = ctypes.c_size_t()
@@ -881,37 +872,31 @@ def ssconv_grad_norm_ws_bytes(tensors: int) -> int:
     return int(n.value)
 
 
-def ssconv_grad_norm(grads, kind: int = GRAD_NORM_L2, norm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
-                     stream=None) -> torch.Tensor:
+@_on_stream
+def ssconv_grad_norm(grads, kind: int = GRAD_NORM_L2, norm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """fp32 [1] on the device: the root of the sum of all squares (GRAD_NORM_L2), or the largest magnitude (GRAD_NORM_INF), of
     a list of fp32 or bf16 tensors (not synchronised)."""
-    b = _binding()
-    if norm is None or ws is None:
-        like = next(iter(grads), norm)
-        if like is None:
-            raise ValueError("without gradients, the norm's tensor has to be given")
-        if norm is None:
-            norm = _new(stream, like, (1,), torch.float32)
-        if ws is None:
-            ws = _new(stream, like, (ssconv_grad_norm_ws_bytes(len(grads)),), torch.uint8)
-    _check("ssconv_grad_norm", b.grad_norm(grads, kind, norm, ws, stream))
+    rc, norm = _binding().grad_norm(grads, kind, norm, ws)
+    _check("ssconv_grad_norm", rc)
     return norm
 
 
-def ssconv_clip_grads(grads, norm: torch.Tensor, max_norm: float, out=None, stream=None):
+@_on_stream
+def ssconv_clip_grads(grads, norm: torch.Tensor, max_norm: float, out=None):
     """Scale every gradient by min(1, max_norm / (norm + 1e-6)), norm as ssconv_grad_norm wrote it: in place, or into the
     tensors of `out` (of the same types); returns the list of results."""
     if out is None:
         out = grads
-    _check("ssconv_clip_grads", _binding().clip_grads(grads, out, norm, max_norm, stream))
+    _check("ssconv_clip_grads", _binding().clip_grads(grads, out, norm, max_norm)[0])
     return out
 
 
+@_on_stream
 def ssconv_adamw_multi(theta, g, m, v, step: int, lr: float = 1.0, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
-                       weight_decay: float = 1e-4, norm: Optional[torch.Tensor] = None, max_norm: float = 1.0, stream=None) -> None:
+                       weight_decay: float = 1e-4, norm: Optional[torch.Tensor] = None, max_norm: float = 1.0) -> None:
     """ssconv_adamw of every tensor of the lists theta, m, v (fp32, modified) with the gradients g (fp32 or bf16); with `norm`
     the gradients are scaled as by ssconv_clip_grads on the way (g itself stays as it is)."""
-    _check("ssconv_adamw_multi", _binding().adamw_multi(theta, g, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm, stream))
+    _check("ssconv_adamw_multi", _binding().adamw_multi(theta, g, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm)[0])
 
 
 # ----------------------------------------------------------------------------- the end of a block
@@ -930,33 +915,15 @@ def make_resnorm(rows: int, C: int, rows_per_gate: int = 0, post: int = NORM_NON
     return ResNorm(rows, rows_per_gate, C, post, pre, scale, eps)
 
 
-def _gates(desc: ResNorm) -> int:
-    """Elements of the gates of a descriptor."""
-    return desc.C * (1 if desc.rows_per_gate == 0 else -(-desc.rows // desc.rows_per_gate))
-
-
+@_on_stream
 def ssconv_residual_norm(desc: ResNorm, x: torch.Tensor, b: torch.Tensor, gate: Optional[torch.Tensor] = None,
                          post_gamma: Optional[torch.Tensor] = None, post_beta: Optional[torch.Tensor] = None,
                          pre_gamma: Optional[torch.Tensor] = None, pre_beta: Optional[torch.Tensor] = None, want_stats: bool = False,
-                         h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
-                         stream=None):
+                         h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None):
     """(h, y or None, stats or None): h = scale x + gate post(b), y = pre(h), bf16 like x; stats fp32 [rows, 4] for the backward
     call.  gate fp32 [C] or [ceil(rows / rows_per_gate), C]; gammas and betas fp32 [C], None for ones and zeros."""
-    n = desc.rows * desc.C
-    for name, t in (("x", x), ("b", b), ("h", h), ("y", y)):
-        _expect(name, t, torch.bfloat16, n)
-    for name, t in (("post_gamma", post_gamma), ("post_beta", post_beta), ("pre_gamma", pre_gamma), ("pre_beta", pre_beta)):
-        _expect(name, t, torch.float32, desc.C)
-    _expect("gate", gate, torch.float32, _gates(desc))
-    _expect("stats", stats, torch.float32, 4 * desc.rows)
-    if h is None:
-        h = _new(stream, x, x.shape, torch.bfloat16)
-    if y is None and desc.pre != NORM_NONE:
-        y = _new(stream, x, x.shape, torch.bfloat16)
-    if stats is None and want_stats:
-        stats = _new(stream, x, (desc.rows, 4), torch.float32)
-    _check("ssconv_residual_norm", _binding().ssconv_residual_norm(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, h, y, stats,
-                                                                   stream))
+    rc, h, y, stats = _binding().residual_norm(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, want_stats, h, y, stats)
+    _check("ssconv_residual_norm", rc)
     return h, y, stats
 
 
@@ -979,33 +946,20 @@ def ssconv_residual_norm_ws_bytes(desc: ResNorm) -> int:
     return int(n.value)
 
 
+@_on_stream
 def ssconv_residual_norm_backward(desc: ResNorm, x: torch.Tensor, b: torch.Tensor, stats: Optional[torch.Tensor],
                                   dh: Optional[torch.Tensor], dy: Optional[torch.Tensor], gate: Optional[torch.Tensor] = None,
                                   post_gamma: Optional[torch.Tensor] = None, post_beta: Optional[torch.Tensor] = None,
                                   pre_gamma: Optional[torch.Tensor] = None, pre_beta: Optional[torch.Tensor] = None,
-                                  ws: Optional[torch.Tensor] = None, stream=None) -> ResNormGrads:
+                                  ws: Optional[torch.Tensor] = None) -> ResNormGrads:
     """Gradients from dh and dy (bf16 like x; dh may be None) and the forward call's inputs and stats: dx, db bf16, the others
     fp32 and of their inputs' shapes, one for each gate, gamma and beta that is given."""
-    n = desc.rows * desc.C
-    for name, t in (("x", x), ("b", b), ("dh", dh), ("dy", dy)):
-        _expect(name, t, torch.bfloat16, n)
-    params = (post_gamma, post_beta, pre_gamma, pre_beta)
-    for name, t in zip(("post_gamma", "post_beta", "pre_gamma", "pre_beta"), params):
-        _expect(name, t, torch.float32, desc.C)
-    _expect("gate", gate, torch.float32, _gates(desc))
-    _expect("stats", stats, torch.float32, 4 * desc.rows)
-    dx, db = (_new(stream, x, x.shape, torch.bfloat16) for _ in range(2))
-    dgate, *sums = (None if t is None else _new(stream, x, t.shape, torch.float32) for t in (gate, *params))
-    if ws is None:
-        ws = _new(stream, x, (max(16, ssconv_residual_norm_ws_bytes(desc)),), torch.uint8)
-    _check("ssconv_residual_norm_backward",
-           _binding().ssconv_residual_norm_backward(desc, x, b, stats, dh, dy, gate, post_gamma, post_beta, pre_gamma, dx, db, dgate, *sums,
-                                                    ws, ws, stream))
-    return ResNormGrads(dx, db, dgate, *sums)
+    rc, *grads = _binding().residual_norm_backward(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, stats, dh, dy, ws)
+    _check("ssconv_residual_norm_backward", rc)
+    return ResNormGrads(*grads)
 
 
 # ----------------------------------------------------------------------------- 4-bit operands with a scale per block
-@functools.lru_cache(maxsize=1024)
 def ssconv_sizes_mxfp4(rows: int, C: int) -> Tuple[int, int]:
     """(code bytes, scale bytes) of rows of C channels in microscaled 4-bit values."""
     a, b = ctypes.c_size_t(), ctypes.c_size_t()
@@ -1013,53 +967,29 @@ def ssconv_sizes_mxfp4(rows: int, C: int) -> Tuple[int, int]:
     return int(a.value), int(b.value)
 
 
-def ssconv_quantize_mxfp4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
+@_on_stream
+def ssconv_quantize_mxfp4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
     """(codes, scales) uint8 of bf16 x [..., C]: e2m1 elements, one power of two per 32 channels; scales in the tile order that
     ssconv_forward_dense_mxfp4 reads.  Weights [C_out, C_in] are quantised by the same call."""
-    C = x.shape[-1]
-    rows = x.numel() // C if C else 0
-    _expect("x", x, torch.bfloat16, rows * C)
-    n_codes, n_scales = ssconv_sizes_mxfp4(rows, C)
-    _expect("codes", codes, torch.uint8, n_codes)
-    _expect("scales", scales, torch.uint8, n_scales)
-    if codes is None:
-        codes = _new(stream, x, (*x.shape[:-1], -(-C // 32) * 16), torch.uint8)
-    if scales is None:
-        scales = _new(stream, x, (n_scales,), torch.uint8)
-    _check("ssconv_quantize_mxfp4", _binding().ssconv_quantize_mxfp4(x, rows, C, codes, scales, stream))
+    rc, codes, scales = _binding().quantize_mxfp4(x, codes, scales)
+    _check("ssconv_quantize_mxfp4", rc)
     return codes, scales
 
 
-def ssconv_dequantize_mxfp4(codes: torch.Tensor, scales: torch.Tensor, C: int, x: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+@_on_stream
+def ssconv_dequantize_mxfp4(codes: torch.Tensor, scales: torch.Tensor, C: int, x: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The bf16 values [..., C] that codes and scales stand for (exact)."""
-    row = -(-C // 32) * 16
-    if C <= 0 or codes.shape[-1] != row:
-        raise ValueError(f"codes: rows of {C} channels are {row} bytes, not {codes.shape[-1]}")
-    rows = codes.numel() // row
-    n_codes, n_scales = ssconv_sizes_mxfp4(rows, C)
-    _expect("codes", codes, torch.uint8, n_codes)
-    _expect("scales", scales, torch.uint8, n_scales)
-    _expect("x", x, torch.bfloat16, rows * C)
-    if x is None:
-        x = _new(stream, codes, (*codes.shape[:-1], C), torch.bfloat16)
-    _check("ssconv_dequantize_mxfp4", _binding().ssconv_dequantize_mxfp4(codes, scales, rows, C, x, stream))
+    rc, x = _binding().dequantize_mxfp4(codes, scales, C, x)
+    _check("ssconv_dequantize_mxfp4", rc)
     return x
 
 
+@_on_stream
 def ssconv_forward_dense_mxfp4(desc: Desc, x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
                                bias: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
-                               dev_status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                               dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Point-wise layer on microscaled 4-bit activations and weights (both from ssconv_quantize_mxfp4); bf16 output
     [N,H,W,C_out] (enqueued, not synchronised)."""
-    pixels = desc.N * desc.H * desc.W
-    (n_xc, n_xs), (n_wc, n_ws) = ssconv_sizes_mxfp4(pixels, desc.C_in), ssconv_sizes_mxfp4(desc.C_out, desc.C_in)
-    for name, t, n in (("x_codes", x_codes, n_xc), ("x_scales", x_scales, n_xs), ("w_codes", w_codes, n_wc), ("w_scales", w_scales, n_ws)):
-        _expect(name, t, torch.uint8, n)
-    _expect("bias", bias, torch.float32, desc.C_out)
-    _expect("y", y, torch.bfloat16, pixels * desc.C_out)
-    _expect("dev_status", dev_status, torch.int32, 1)
-    if y is None:
-        y = _new(stream, x_codes, (desc.N, desc.H, desc.W, desc.C_out), torch.bfloat16)
-    _check("ssconv_forward_dense_mxfp4",
-           _binding().ssconv_forward_dense_mxfp4(desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status, stream))
+    rc, y = _binding().forward_dense_mxfp4(desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status)
+    _check("ssconv_forward_dense_mxfp4", rc)
     return y

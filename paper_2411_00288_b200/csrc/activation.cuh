@@ -22,17 +22,9 @@ constexpr float kGeluC1 = 1.1512105857193118f, kGeluC2 = -0.4585589426410932f, k
                 kGeluC4 = 0.008460201316438069f, kGeluC5 = 0.0009178260683469985f, kGeluC6 = 5.989503356838717e-05f,
                 kGeluC7 = 1.7442654864735877e-06f;
 // Two values at once, the polynomial on fp32 pairs (fma.rn.f32x2).
-__device__ __forceinline__ unsigned long long f32x2(float lo, float hi) {
-  unsigned long long r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
 __device__ __forceinline__ unsigned long long horner2(unsigned long long r, unsigned long long z, float c) {
   asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(r) : "l"(z), "l"(f32x2(c, c)));
   return r;
-}
-__device__ __forceinline__ void split2(unsigned long long v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
 }
 __device__ __forceinline__ unsigned long long gelu_f32x2(unsigned long long x) {
   float lo, hi;

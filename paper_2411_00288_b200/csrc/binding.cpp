@@ -148,12 +148,96 @@ PyObject* blob(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// The calls over many tensors: lists (or tuples) of contiguous fp32 tensors, or bf16 ones where the call takes them, on the
-// current device, as many and of the same extents in each list.
+// ---- Calls that also check and allocate their tensors here: as much Python as the call itself takes would double its time.
+// (Outputs that are not given are allocated for the current stream.)
+
+bool here(const at::Tensor& t) { return t.is_cuda() && t.is_contiguous() && t.get_device() == c10::cuda::current_device(); }
+
+// The address of a tensor of `numel` elements of `type` on the current device, or nullptr for None.
+void* expect(PyObject* o, const char* name, at::ScalarType type, int64_t numel) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = as_tensor(o);
+  if (t.scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "%s: %s is expected, not %s", name, c10::toString(type), c10::toString(t.scalar_type()));
+    throw PythonError{};
+  }
+  if (t.numel() != numel) {
+    PyErr_Format(PyExc_ValueError, "%s: %lld elements are expected, not %lld", name, (long long)numel, (long long)t.numel());
+    throw PythonError{};
+  }
+  if (!here(t)) {
+    PyErr_Format(PyExc_ValueError, "%s: tensors must be contiguous and on the current CUDA device", name);
+    throw PythonError{};
+  }
+  return t.mutable_data_ptr();
+}
+
+// A new tensor beside `like` if o is None, o itself otherwise (checked by expect()).
+at::Tensor given_or_new(PyObject* o, at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
+  if (o != Py_None) return as_tensor(o);
+  return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+}
+void* address(const at::Tensor& t) { return t.numel() != 0 ? t.mutable_data_ptr() : nullptr; }
+
+// (status, results...): what a call gives back to its Python function.
+template <class... T>
+PyObject* results(int32_t rc, const T&... tensors) {
+  PyObject* out = PyTuple_New(1 + sizeof...(T));
+  if (out == nullptr) throw PythonError{};
+  PyTuple_SET_ITEM(out, 0, PyLong_FromLong(rc));
+  Py_ssize_t i = 1;
+  const auto put = [&](const at::Tensor& t) {
+    if (t.defined()) {
+      PyTuple_SET_ITEM(out, i++, THPVariable_Wrap(t));
+    } else {
+      Py_INCREF(Py_None);
+      PyTuple_SET_ITEM(out, i++, Py_None);
+    }
+  };
+  (put(tensors), ...);
+  return out;
+}
+
+template <class F>
+int32_t without_gil(F f) {
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f();
+  Py_END_ALLOW_THREADS
+  return rc;
+}
+
+void* current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
+
+double as_double(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw PythonError{};
+  return v;
+}
+
+// The body of such a call: its arguments are counted, its exceptions become Python's.
+template <PyObject* (*BODY)(PyObject* const*)>
+PyObject* checked(PyObject* const* args, Py_ssize_t n, Py_ssize_t expected) {
+  HANDLE_TH_ERRORS
+  if (n != expected) {
+    PyErr_Format(PyExc_TypeError, "%zd arguments, %zd expected", n, expected);
+    return nullptr;
+  }
+  try {
+    return BODY(args);
+  } catch (const PythonError&) {
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// Lists (or tuples) of contiguous fp32 tensors, or bf16 ones where the call takes them, on the current device, as many and of the
+// same extents in each list.
 struct TensorList {
   std::vector<void*> p;
   std::vector<int64_t> n;
   std::vector<int32_t> type;
+  at::Tensor first;  // (undefined: an empty list)
   TensorList(PyObject* o, bool takes_bf16, const TensorList* like) {
     PyObject* items = PySequence_Fast(o, "a list of tensors is expected");
     if (items == nullptr) throw PythonError{};
@@ -162,119 +246,239 @@ struct TensorList {
       ~Release() { Py_DECREF(o); }
     } release{items};
     const Py_ssize_t count = PySequence_Fast_GET_SIZE(items);
+    if (count > INT32_MAX) raise(PyExc_ValueError, "too many tensors");
     if (like != nullptr && (size_t)count != like->n.size()) raise(PyExc_ValueError, "the lists have different lengths");
     p.reserve(count);
     n.reserve(count);
     type.reserve(count);
     for (Py_ssize_t i = 0; i < count; ++i) {
       const at::Tensor& t = as_tensor(PySequence_Fast_GET_ITEM(items, i));
-      if (!t.is_cuda() || !t.is_contiguous() || t.get_device() != c10::cuda::current_device())
-        raise(PyExc_ValueError, "tensors must be contiguous and on the current CUDA device");
+      if (!here(t)) raise(PyExc_ValueError, "tensors must be contiguous and on the current CUDA device");
       const bool bf16 = t.scalar_type() == at::kBFloat16;
       if (!bf16 && t.scalar_type() != at::kFloat) raise(PyExc_TypeError, "float32 or bfloat16 tensors are expected");
       if (bf16 && !takes_bf16) raise(PyExc_TypeError, "float32 tensors are expected");
       if (like != nullptr && t.numel() != like->n[i]) raise(PyExc_ValueError, "tensors of one position have different extents");
-      p.push_back(t.numel() != 0 ? t.mutable_data_ptr() : nullptr);
+      if (i == 0) first = t;
+      p.push_back(address(t));
       n.push_back(t.numel());
       type.push_back(bf16 ? SSCONV_BF16 : SSCONV_F32);
     }
-    if (count > INT32_MAX) raise(PyExc_ValueError, "too many tensors");
   }
   int32_t size() const { return (int32_t)p.size(); }
 };
-const float* as_norm(PyObject* o) {
-  if (o == Py_None) return nullptr;
-  const at::Tensor& t = as_tensor(o);
-  if (!t.is_cuda() || t.numel() != 1 || t.scalar_type() != at::kFloat || t.get_device() != c10::cuda::current_device())
-    raise(PyExc_ValueError, "the norm is one float32 number on the current CUDA device");
-  return static_cast<const float*>(t.mutable_data_ptr());
-}
-double as_double(PyObject* o) {
-  const double v = PyFloat_AsDouble(o);
-  if (v == -1.0 && PyErr_Occurred()) throw PythonError{};
-  return v;
+
+// grad_norm(grads, kind, norm, ws) -> (status, norm)
+PyObject* grad_norm(PyObject* const* a) {
+  const TensorList g(a[0], true, nullptr);
+  const int32_t kind = (int32_t)as_int(a[1]);
+  expect(a[2], "norm", at::kFloat, 1);
+  if (!g.first.defined() && (a[2] == Py_None || a[3] == Py_None))
+    raise(PyExc_ValueError, "without gradients the norm's tensor and the scratch have to be given");
+  at::Tensor norm = given_or_new(a[2], {1}, at::kFloat, g.first), ws;
+  if (a[3] != Py_None) {
+    ws = as_tensor(a[3]);
+    expect(a[3], "ws", ws.scalar_type(), ws.numel());
+  } else {
+    size_t bytes = 0;
+    const int32_t rc = ssconv_grad_norm_ws_bytes(g.size(), &bytes);
+    if (rc != SSCONV_OK) return results(rc, at::Tensor());
+    ws = given_or_new(Py_None, {(int64_t)bytes}, at::kByte, g.first);
+  }
+  void* stream = current_stream();
+  return results(without_gil([&] {
+                   return ssconv_grad_norm(g.p.data(), g.n.data(), g.type.data(), g.size(), kind, static_cast<float*>(address(norm)), address(ws),
+                                           ws.nbytes(), stream);
+                 }),
+                 norm);
 }
 
-// grad_norm(grads, kind, norm, ws, stream)
-PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  HANDLE_TH_ERRORS
-  try {
-    if (n != 5) raise(PyExc_TypeError, "grad_norm(grads, kind, norm, ws, stream)");
-    const TensorList g(args[0], true, nullptr);
-    const int32_t kind = (int32_t)as_int(args[1]);
-    float* norm = const_cast<float*>(as_norm(args[2]));
-    void* ws = as_address(args[3]);
-    const size_t ws_bytes = args[3] == Py_None ? 0 : as_tensor(args[3]).nbytes();
-    void* stream = as_stream(args[4]);
-    int32_t rc;
-    Py_BEGIN_ALLOW_THREADS
-    rc = ssconv_grad_norm(g.p.data(), g.n.data(), g.type.data(), g.size(), kind, norm, ws, ws_bytes, stream);
-    Py_END_ALLOW_THREADS
-    return PyLong_FromLong(rc);
-  } catch (const PythonError&) {
-    return nullptr;
-  }
-  END_HANDLE_TH_ERRORS
+// clip_grads(grads, out, norm, max_norm) -> (status,)
+PyObject* clip_grads(PyObject* const* a) {
+  const TensorList g(a[0], true, nullptr), out(a[1], true, &g);
+  if (g.type != out.type) raise(PyExc_TypeError, "a gradient and its output have different types");
+  const float* norm = static_cast<const float*>(expect(a[2], "norm", at::kFloat, 1));
+  const float max_norm = (float)as_double(a[3]);
+  void* stream = current_stream();
+  return results(without_gil(
+      [&] { return ssconv_clip_grads(g.p.data(), out.p.data(), g.n.data(), g.type.data(), g.size(), norm, max_norm, stream); }));
 }
 
-// clip_grads(grads, out, norm, max_norm, stream)
-PyObject* clip_grads(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  HANDLE_TH_ERRORS
-  try {
-    if (n != 5) raise(PyExc_TypeError, "clip_grads(grads, out, norm, max_norm, stream)");
-    const TensorList g(args[0], true, nullptr), out(args[1], true, &g);
-    if (g.type != out.type) raise(PyExc_TypeError, "a gradient and its output have different types");
-    const float* norm = as_norm(args[2]);
-    const float max_norm = (float)as_double(args[3]);
-    void* stream = as_stream(args[4]);
-    int32_t rc;
-    Py_BEGIN_ALLOW_THREADS
-    rc = ssconv_clip_grads(g.p.data(), out.p.data(), g.n.data(), g.type.data(), g.size(), norm, max_norm, stream);
-    Py_END_ALLOW_THREADS
-    return PyLong_FromLong(rc);
-  } catch (const PythonError&) {
-    return nullptr;
-  }
-  END_HANDLE_TH_ERRORS
+// adamw_multi(theta, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm) -> (status,)
+PyObject* adamw_multi(PyObject* const* a) {
+  const TensorList g(a[1], true, nullptr), theta(a[0], false, &g), m(a[2], false, &g), v(a[3], false, &g);
+  const int64_t step = as_int(a[4]);
+  if (step < 1 || step > INT32_MAX) raise(PyExc_ValueError, "steps count from 1");
+  const double lr = as_double(a[5]), beta1 = as_double(a[6]), beta2 = as_double(a[7]), eps = as_double(a[8]), decay = as_double(a[9]);
+  const float* norm = static_cast<const float*>(expect(a[10], "norm", at::kFloat, 1));
+  const float max_norm = (float)as_double(a[11]);
+  void* stream = current_stream();
+  return results(without_gil([&] {
+    return ssconv_adamw_multi(theta.p.data(), g.p.data(), m.p.data(), v.p.data(), g.n.data(), g.type.data(), g.size(), (int32_t)step, lr, beta1,
+                              beta2, eps, decay, norm, max_norm, stream);
+  }));
 }
 
-// adamw_multi(theta, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm, stream)
-PyObject* adamw_multi(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  HANDLE_TH_ERRORS
-  try {
-    if (n != 13) raise(PyExc_TypeError, "adamw_multi(theta, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm, stream)");
-    const TensorList g(args[1], true, nullptr), theta(args[0], false, &g), m(args[2], false, &g), v(args[3], false, &g);
-    const int64_t step = as_int(args[4]);
-    if (step < 1 || step > INT32_MAX) raise(PyExc_ValueError, "steps count from 1");
-    const double lr = as_double(args[5]), beta1 = as_double(args[6]), beta2 = as_double(args[7]), eps = as_double(args[8]),
-                 decay = as_double(args[9]);
-    const float* norm = as_norm(args[10]);
-    const float max_norm = (float)as_double(args[11]);
-    void* stream = as_stream(args[12]);
-    int32_t rc;
-    Py_BEGIN_ALLOW_THREADS
-    rc = ssconv_adamw_multi(theta.p.data(), g.p.data(), m.p.data(), v.p.data(), g.n.data(), g.type.data(), g.size(), (int32_t)step, lr, beta1,
-                            beta2, eps, decay, norm, max_norm, stream);
-    Py_END_ALLOW_THREADS
-    return PyLong_FromLong(rc);
-  } catch (const PythonError&) {
-    return nullptr;
+int64_t elements(const ssconv_resnorm_t& d) { return d.rows * d.C; }
+// (of a descriptor that the library refuses any number will do: nothing is allocated by it)
+int64_t gates(const ssconv_resnorm_t& d) {
+  return d.rows_per_gate > 0 ? (d.rows + d.rows_per_gate - 1) / d.rows_per_gate * d.C : d.C;
+}
+
+struct ResNormInputs {
+  Held held;
+  const ssconv_resnorm_t* d;
+  void *x, *b;
+  float *gate, *post_gamma, *post_beta, *pre_gamma, *pre_beta;
+  // desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta
+  explicit ResNormInputs(PyObject* const* a) {
+    d = convert<const ssconv_resnorm_t*>(a[0], held, false);
+    x = expect(a[1], "x", at::kBFloat16, elements(*d));
+    b = expect(a[2], "b", at::kBFloat16, elements(*d));
+    if (a[1] == Py_None) raise(PyExc_TypeError, "x: a tensor is expected");
+    gate = static_cast<float*>(expect(a[3], "gate", at::kFloat, gates(*d)));
+    post_gamma = static_cast<float*>(expect(a[4], "post_gamma", at::kFloat, d->C));
+    post_beta = static_cast<float*>(expect(a[5], "post_beta", at::kFloat, d->C));
+    pre_gamma = static_cast<float*>(expect(a[6], "pre_gamma", at::kFloat, d->C));
+    pre_beta = static_cast<float*>(expect(a[7], "pre_beta", at::kFloat, d->C));
   }
-  END_HANDLE_TH_ERRORS
+};
+
+// residual_norm(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, want_stats, h, y, stats) -> (status, h, y, stats)
+PyObject* residual_norm(PyObject* const* a) {
+  const ResNormInputs in(a);
+  const ssconv_resnorm_t& d = *in.d;
+  const at::Tensor& x = as_tensor(a[1]);
+  expect(a[9], "h", at::kBFloat16, elements(d));
+  expect(a[10], "y", at::kBFloat16, elements(d));
+  expect(a[11], "stats", at::kFloat, 4 * d.rows);
+  const int want_stats = PyObject_IsTrue(a[8]);
+  if (want_stats < 0) throw PythonError{};
+  at::Tensor h = given_or_new(a[9], x.sizes(), at::kBFloat16, x), y, stats;
+  if (a[10] != Py_None || d.pre != SSCONV_NORM_NONE) y = given_or_new(a[10], x.sizes(), at::kBFloat16, x);
+  if (a[11] != Py_None || want_stats) stats = given_or_new(a[11], {d.rows, 4}, at::kFloat, x);
+  void* stream = current_stream();
+  const int32_t rc = without_gil([&] {
+    return ssconv_residual_norm(&d, in.x, in.b, in.gate, in.post_gamma, in.post_beta, in.pre_gamma, in.pre_beta, address(h),
+                                y.defined() ? address(y) : nullptr, stats.defined() ? static_cast<float*>(address(stats)) : nullptr, stream);
+  });
+  return results(rc, h, y, stats);
+}
+
+// residual_norm_backward(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, stats, dh, dy, ws)
+//   -> (status, dx, db, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta)
+PyObject* residual_norm_backward(PyObject* const* a) {
+  const ResNormInputs in(a);
+  const ssconv_resnorm_t& d = *in.d;
+  const at::Tensor& x = as_tensor(a[1]);
+  const float* stats = static_cast<const float*>(expect(a[8], "stats", at::kFloat, 4 * d.rows));
+  const void* dh = expect(a[9], "dh", at::kBFloat16, elements(d));
+  const void* dy = expect(a[10], "dy", at::kBFloat16, elements(d));
+  at::Tensor dx = given_or_new(Py_None, x.sizes(), at::kBFloat16, x), db = given_or_new(Py_None, x.sizes(), at::kBFloat16, x), sums[5], ws;
+  float* out[5];
+  for (int i = 0; i < 5; ++i) {
+    if (a[3 + i] != Py_None) sums[i] = given_or_new(Py_None, as_tensor(a[3 + i]).sizes(), at::kFloat, x);
+    out[i] = sums[i].defined() ? static_cast<float*>(address(sums[i])) : nullptr;
+  }
+  if (a[11] != Py_None) {
+    ws = as_tensor(a[11]);
+    expect(a[11], "ws", ws.scalar_type(), ws.numel());
+  } else {
+    size_t bytes = 0;
+    const int32_t rc = ssconv_residual_norm_ws_bytes(&d, &bytes);
+    if (rc != SSCONV_OK) return results(rc, dx, db, sums[0], sums[1], sums[2], sums[3], sums[4]);
+    ws = given_or_new(Py_None, {(int64_t)bytes}, at::kByte, x);
+  }
+  void* stream = current_stream();
+  const int32_t rc = without_gil([&] {
+    return ssconv_residual_norm_backward(&d, in.x, in.b, stats, dh, dy, in.gate, in.post_gamma, in.post_beta, in.pre_gamma, address(dx), address(db),
+                                         out[0], out[1], out[2], out[3], out[4], address(ws), ws.nbytes(), stream);
+  });
+  return results(rc, dx, db, sums[0], sums[1], sums[2], sums[3], sums[4]);
+}
+
+std::vector<int64_t> with_last(const at::Tensor& t, int64_t last) {
+  std::vector<int64_t> shape(t.sizes().begin(), t.sizes().end());
+  shape.back() = last;
+  return shape;
+}
+
+// quantize_mxfp4(x, codes, scales) -> (status, codes, scales)
+PyObject* quantize_mxfp4(PyObject* const* a) {
+  const at::Tensor& x = as_tensor(a[0]);
+  if (x.dim() == 0) raise(PyExc_ValueError, "x: rows of channels are expected");
+  const int64_t C = x.size(-1), rows = C > 0 ? x.numel() / C : 0;
+  void* px = expect(a[0], "x", at::kBFloat16, rows * C);
+  if (C > INT32_MAX) raise(PyExc_ValueError, "x: too many channels");
+  size_t n_codes = 0, n_scales = 0;
+  const int32_t sized = ssconv_sizes_mxfp4(rows, (int32_t)C, &n_codes, &n_scales);
+  if (sized != SSCONV_OK) return results(sized, at::Tensor(), at::Tensor());
+  expect(a[1], "codes", at::kByte, (int64_t)n_codes);
+  expect(a[2], "scales", at::kByte, (int64_t)n_scales);
+  const at::Tensor codes = given_or_new(a[1], with_last(x, (C + 31) / 32 * 16), at::kByte, x), scales = given_or_new(a[2], {(int64_t)n_scales}, at::kByte, x);
+  void* stream = current_stream();
+  const int32_t rc = without_gil([&] { return ssconv_quantize_mxfp4(px, rows, (int32_t)C, address(codes), address(scales), stream); });
+  return results(rc, codes, scales);
+}
+
+// dequantize_mxfp4(codes, scales, C, x) -> (status, x)
+PyObject* dequantize_mxfp4(PyObject* const* a) {
+  const at::Tensor& codes = as_tensor(a[0]);
+  const int64_t C = as_int(a[2]);
+  if (C <= 0 || C > INT32_MAX) raise(PyExc_ValueError, "C: a positive number of channels is expected");
+  const int64_t row = (C + 31) / 32 * 16;
+  if (codes.dim() == 0 || codes.size(-1) != row) {
+    PyErr_Format(PyExc_ValueError, "codes: rows of %lld channels are %lld bytes", (long long)C, (long long)row);
+    throw PythonError{};
+  }
+  const int64_t rows = codes.numel() / row;
+  size_t n_codes = 0, n_scales = 0;
+  const int32_t sized = ssconv_sizes_mxfp4(rows, (int32_t)C, &n_codes, &n_scales);
+  if (sized != SSCONV_OK) return results(sized, at::Tensor());
+  void* pc = expect(a[0], "codes", at::kByte, (int64_t)n_codes);
+  void* ps = expect(a[1], "scales", at::kByte, (int64_t)n_scales);
+  expect(a[3], "x", at::kBFloat16, rows * C);
+  const at::Tensor x = given_or_new(a[3], with_last(codes, C), at::kBFloat16, codes);
+  void* stream = current_stream();
+  return results(without_gil([&] { return ssconv_dequantize_mxfp4(pc, ps, rows, (int32_t)C, address(x), stream); }), x);
+}
+
+// forward_dense_mxfp4(desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status) -> (status, y)
+PyObject* forward_dense_mxfp4(PyObject* const* a) {
+  Held held;
+  const ssconv_desc_t& d = *convert<const ssconv_desc_t*>(a[0], held, false);
+  const int64_t pixels = (int64_t)d.N * d.H * d.W;
+  size_t n[4];
+  int32_t rc = ssconv_sizes_mxfp4(pixels, d.C_in, &n[0], &n[1]);
+  if (rc == SSCONV_OK) rc = ssconv_sizes_mxfp4(d.C_out, d.C_in, &n[2], &n[3]);
+  if (rc != SSCONV_OK) return results(rc, at::Tensor());
+  static const char* const names[4] = {"x_codes", "x_scales", "w_codes", "w_scales"};
+  void* p[4];
+  for (int i = 0; i < 4; ++i) p[i] = expect(a[1 + i], names[i], at::kByte, (int64_t)n[i]);
+  const float* bias = static_cast<const float*>(expect(a[5], "bias", at::kFloat, d.C_out));
+  expect(a[6], "y", at::kBFloat16, pixels * d.C_out);
+  int32_t* status = static_cast<int32_t*>(expect(a[7], "dev_status", at::kInt, 1));
+  const at::Tensor y = given_or_new(a[6], {d.N, d.H, d.W, d.C_out}, at::kBFloat16, as_tensor(a[1]));
+  void* stream = current_stream();
+  rc = without_gil([&] { return ssconv_forward_dense_mxfp4(&d, p[0], p[1], p[2], p[3], bias, address(y), status, stream); });
+  return results(rc, y);
+}
+
+template <PyObject* (*BODY)(PyObject* const*), Py_ssize_t COUNT>
+PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return checked<BODY>(args, n, COUNT);
 }
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))Entry<&name>::call, METH_FASTCALL, nullptr}
+#define CALL(name, count) {#name, (PyCFunction)(void (*)(void))call<name, count>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     ENTRY(ssconv_select_mask), ENTRY(ssconv_compress), ENTRY(ssconv_maxpool), ENTRY(ssconv_space_to_depth),
     ENTRY(ssconv_forward), ENTRY(ssconv_forward_res), ENTRY(ssconv_forward_dense), ENTRY(ssconv_forward_dense_res),
     ENTRY(ssconv_forward_dense_strided), ENTRY(ssconv_soft_mask), ENTRY(ssconv_mask_grad), ENTRY(ssconv_adamw),
     ENTRY(ssconv_wgrad), ENTRY(ssconv_dgrad), ENTRY(ssconv_forward_grouped), ENTRY(ssconv_forward_dense_grouped),
     ENTRY(ssconv_depthwise), ENTRY(ssconv_layernorm), ENTRY(ssconv_quantize_e4m3), ENTRY(ssconv_forward_fp8),
-    ENTRY(ssconv_forward_dense_fp8), ENTRY(ssconv_residual_norm), ENTRY(ssconv_residual_norm_backward),
-    ENTRY(ssconv_quantize_mxfp4), ENTRY(ssconv_dequantize_mxfp4), ENTRY(ssconv_forward_dense_mxfp4),
-    {"grad_norm", (PyCFunction)(void (*)(void))grad_norm, METH_FASTCALL, nullptr},
-    {"clip_grads", (PyCFunction)(void (*)(void))clip_grads, METH_FASTCALL, nullptr},
-    {"adamw_multi", (PyCFunction)(void (*)(void))adamw_multi, METH_FASTCALL, nullptr},
+    ENTRY(ssconv_forward_dense_fp8),
+    CALL(grad_norm, 4), CALL(clip_grads, 4), CALL(adamw_multi, 12), CALL(residual_norm, 12), CALL(residual_norm_backward, 12),
+    CALL(quantize_mxfp4, 3), CALL(dequantize_mxfp4, 4), CALL(forward_dense_mxfp4, 8),
     {"output", (PyCFunction)(void (*)(void))output, METH_FASTCALL, nullptr},
     {"blob", (PyCFunction)(void (*)(void))blob, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

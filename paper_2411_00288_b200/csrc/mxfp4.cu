@@ -16,8 +16,9 @@ namespace {
 // ---------------------------------------------------------------------------------------
 // Quantisation.  The scale's exponent comes from the exponent field E of the block's largest magnitude: floor(log2) = E - 127, so
 // the code (bias 127) is E - 2, at least 0; E = 255 (an infinity or a NaN) gives 255.  Elements are multiplied by the inverse
-// power of two (exact) and rounded once.  Four lanes hold a block, 16 lanes a row's share of a scale image.  DRAM-bound:
-// 2.53 bytes per element.
+// power of two (exact) and rounded once.  A thread block takes the 128 rows x 128 channels of a scale image, 16 lanes a row and
+// four lanes a block of 32, each thread eight rows: eight loads in flight, and the image is written whole.  DRAM-bound: 2.53
+// bytes per element.
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, float scale) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -40,29 +41,41 @@ __device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, float scale) {
 }
 __device__ __forceinline__ uint32_t magnitude_bits(uint32_t pair) { return max(pair & 0x7FFFu, (pair >> 16) & 0x7FFFu); }
 
-__global__ void __launch_bounds__(256) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint32_t* scales, uint32_t rows, uint32_t items,
-                                                             uint32_t chunks, uint32_t blocks, uint32_t C8) {
+constexpr int kMxRowsPerThread = 8;  // 16 rows of threads
+
+__global__ void __launch_bounds__(256) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint4* scales, uint32_t rows, uint32_t chunks,
+                                                             uint32_t blocks, uint32_t C8) {
+  __shared__ __align__(16) uint32_t image[128];
   grid_launch_dependents();
-  const uint32_t item = blockIdx.x * 16u + (threadIdx.x >> 4);  // (row, chunk)
-  const uint32_t lane = threadIdx.x & 15u;
-  const uint32_t row = item / chunks, chunk = item - row * chunks;
-  grid_dependency_wait();
-  if (item >= items) return;  // (whole halves of a warp: the shuffles below stay among 16 lanes)
-  const uint32_t mask = 0xFFFFu << (threadIdx.x & 16u);
+  const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
+  const uint32_t lane = threadIdx.x & 15u, r0 = threadIdx.x >> 4;
   const uint32_t piece = chunk * 16u + lane;  // of 8 channels
-  uint4 v = make_uint4(0u, 0u, 0u, 0u);
-  if (row < rows && piece < C8) v = x[(uint64_t)row * C8 + piece];
-  uint32_t m = max(max(magnitude_bits(v.x), magnitude_bits(v.y)), max(magnitude_bits(v.z), magnitude_bits(v.w)));
-  m = max(m, __shfl_xor_sync(mask, m, 1));
-  m = max(m, __shfl_xor_sync(mask, m, 2));
-  const uint32_t e = m >> 7;
-  const uint32_t code = e == 255u ? 255u : e < 2u ? 0u : e - 2u;
-  const float inverse = __uint_as_float((254u - min(code, 252u)) << 23);
-  if (row < rows && (piece >> 2) < blocks) codes[(uint64_t)row * (4u * blocks) + piece] = e2m1_x8(v, inverse);
-  uint32_t word = code << (8u * (lane >> 2));
-  word |= __shfl_xor_sync(mask, word, 4);
-  word |= __shfl_xor_sync(mask, word, 8);
-  if (lane == 0) scales[((uint64_t)(row >> 7) * chunks + chunk) * 128u + (row & 31u) * 4u + ((row >> 5) & 3u)] = word;
+  const uint32_t there = rows - tile * 128u;  // rows from the tile's first on
+  grid_dependency_wait();
+  uint4 v[kMxRowsPerThread];
+#pragma unroll
+  for (int u = 0; u < kMxRowsPerThread; ++u) {
+    const uint32_t r = r0 + 16u * u;
+    v[u] = make_uint4(0u, 0u, 0u, 0u);
+    if (r < there && piece < C8) v[u] = x[(uint64_t)(tile * 128u + r) * C8 + piece];
+  }
+#pragma unroll
+  for (int u = 0; u < kMxRowsPerThread; ++u) {
+    const uint32_t r = r0 + 16u * u;
+    uint32_t m = max(max(magnitude_bits(v[u].x), magnitude_bits(v[u].y)), max(magnitude_bits(v[u].z), magnitude_bits(v[u].w)));
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+    const uint32_t e = m >> 7;
+    const uint32_t code = e == 255u ? 255u : e < 2u ? 0u : e - 2u;
+    const float inverse = __uint_as_float((254u - min(code, 252u)) << 23);
+    if (r < there && (piece >> 2) < blocks) codes[(uint64_t)(tile * 128u + r) * (4u * blocks) + piece] = e2m1_x8(v[u], inverse);
+    uint32_t word = code << (8u * (lane >> 2));
+    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
+    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
+    if (lane == 0) image[(r & 31u) * 4u + (r >> 5)] = word;
+  }
+  __syncthreads();
+  if (threadIdx.x < 32) scales[(uint64_t)blockIdx.x * 32u + threadIdx.x] = reinterpret_cast<const uint4*>(image)[threadIdx.x];
 }
 
 // The values of codes: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, times the scale; exact in bf16.
@@ -71,31 +84,49 @@ __device__ __forceinline__ float e2m1_value(uint32_t code) {
   const uint32_t bits = e ? ((e + 126u) << 23) | (m << 22) : m * 0x3F000000u;
   return __uint_as_float(bits | ((code & 8u) << 28));
 }
-__global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint64_t pieces, uint32_t C8,
-                                                               uint32_t chunks, uint32_t blocks) {
+__global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint32_t rows, uint32_t chunks,
+                                                               uint32_t blocks, uint32_t C8) {
   grid_launch_dependents();
-  const uint64_t i = blockIdx.x * (uint64_t)blockDim.x + threadIdx.x;
+  const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
+  const uint32_t lane = threadIdx.x & 15u, r0 = threadIdx.x >> 4;
+  const uint32_t piece = chunk * 16u + lane;
+  const uint32_t there = rows - tile * 128u;
   grid_dependency_wait();
-  if (i >= pieces) return;
-  const uint64_t row = i / C8;
-  const uint32_t piece = (uint32_t)(i - row * C8), block = piece >> 2;
-  const uint32_t s = scales[((row >> 7) * chunks + (block >> 2)) * 512u + (row & 31u) * 16u + ((row >> 5) & 3u) * 4u + (block & 3u)];
-  const float scale = __uint_as_float(s == 255u ? 0x7FC00000u : s == 0u ? 0x00400000u : s << 23);
-  const uint32_t c = codes[row * (4u * blocks) + piece];
-  float f[8];
+  if (piece >= C8) return;
+  uint32_t c[kMxRowsPerThread], s[kMxRowsPerThread];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = e2m1_value(c >> (4 * j)) * scale;
-  x[i] = make_uint4(pack_bf16x2<false>(f[0], f[1]), pack_bf16x2<false>(f[2], f[3]), pack_bf16x2<false>(f[4], f[5]), pack_bf16x2<false>(f[6], f[7]));
+  for (int u = 0; u < kMxRowsPerThread; ++u) {
+    const uint32_t r = r0 + 16u * u;
+    c[u] = s[u] = 0u;
+    if (r < there) {
+      c[u] = codes[(uint64_t)(tile * 128u + r) * (4u * blocks) + piece];
+      s[u] = scales[(uint64_t)blockIdx.x * 512u + (r & 31u) * 16u + (r >> 5) * 4u + (lane >> 2)];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kMxRowsPerThread; ++u) {
+    const uint32_t r = r0 + 16u * u;
+    const float scale = __uint_as_float(s[u] == 255u ? 0x7FC00000u : s[u] == 0u ? 0x00400000u : s[u] << 23);
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = e2m1_value(c[u] >> (4 * j)) * scale;
+    if (r < there)
+      x[(uint64_t)(tile * 128u + r) * C8 + piece] =
+          make_uint4(pack_bf16x2<false>(f[0], f[1]), pack_bf16x2<false>(f[2], f[3]), pack_bf16x2<false>(f[4], f[5]), pack_bf16x2<false>(f[6], f[7]));
+  }
 }
 
 // ---------------------------------------------------------------------------------------
 // Product.  y[p, co] = act(bias[co] + sum_ci x_q[p, ci] w_q[co, ci]): tiles of 128 pixels (the accumulator's rows) x BN channels,
 // K in stages of 256 channels (128 bytes of codes per row, the 128-byte swizzle; two scale images per 128 rows).  One thread block
 // per SM walks over tiles, channels first, so that the blocks at work at a time share few rows of x; two accumulators, so that a
-// tile's epilogue runs beside the next one's MMAs.  Warps 0-3 epilogue, 4 producer, 5 MMA issuer.
+// tile's epilogue runs beside the next one's MMAs.  The epilogue's pieces (64 channels) go to kMxSets sets of four warps in turn;
+// two more warps are the producer and the MMA issuer.
 // ---------------------------------------------------------------------------------------
 constexpr long long kMxWaitLimit = 4000000000LL;  // cycles: about 2 s
-constexpr int kMxThreads = 192;
+constexpr int kMxSets = 3;
+constexpr int kMxProducer = 4 * kMxSets, kMxIssuer = kMxProducer + 1;  // warps
+constexpr int kMxThreads = 32 * (kMxIssuer + 1);
 constexpr int kMxStoreBytes = 128 * 128;          // staged outputs: 128 pixels x 64 channels of bf16
 constexpr int kMxMostSmem = 227 * 1024;
 
@@ -104,11 +135,11 @@ struct MxTile {
   static constexpr int kScaleTiles = BN > 128 ? 2 : 1;  // images along the tile's channels
   static constexpr int kBytesA = 128 * 128, kBytesB = BN * 128, kBytesScales = 1024 * (1 + kScaleTiles);
   static constexpr int kBytes = kBytesA + kBytesB + kBytesScales;
-  static constexpr int kRoom = kMxMostSmem - 1024 - 2 * kMxStoreBytes - 256;
+  static constexpr int kRoom = kMxMostSmem - 1024 - kMxSets * kMxStoreBytes - 256;
   static constexpr int kStages = kRoom / kBytes < 6 ? kRoom / kBytes : 6;
   static constexpr int kScaleColumns = 8 * (1 + kScaleTiles);  // of TMEM, per stage: two images of x, two (four) of w
   static constexpr int kTmem = 2 * BN + kStages * kScaleColumns <= 256 ? 256 : 512;
-  static constexpr int kSmem = 1024 + kStages * kBytes + 2 * kMxStoreBytes + 256;
+  static constexpr int kSmem = 1024 + kStages * kBytes + kMxSets * kMxStoreBytes + 256;
   static_assert(2 * BN + kStages * kScaleColumns <= 512 && kStages >= 3, "");
 };
 
@@ -162,8 +193,8 @@ __device__ __forceinline__ void tc_ld_32x32b_x32(uint32_t taddr, uint32_t (&r)[3
       : "r"(taddr)
       : "memory");
 }
-__device__ __forceinline__ void epilogue_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_group_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+// The four warps of a set.
+__device__ __forceinline__ void set_barrier(int set) { asm volatile("bar.sync %0, 128;" ::"r"(1 + set) : "memory"); }
 
 template <int BN, int ACT>
 __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
@@ -174,7 +205,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
   uint8_t* ring_a = smem;
   uint8_t* ring_b = ring_a + T::kStages * T::kBytesA;
   uint8_t* staged = ring_b + T::kStages * T::kBytesB;
-  uint8_t* ring_s = staged + 2 * kMxStoreBytes;
+  uint8_t* ring_s = staged + kMxSets * kMxStoreBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring_s + T::kStages * T::kBytesScales);
   uint64_t *full = bars, *empty = bars + T::kStages, *acc_full = bars + 2 * T::kStages, *acc_empty = acc_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
@@ -189,17 +220,17 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(acc_full + i, 1);
-      mbar_init(acc_empty + i, 4);
+      mbar_init(acc_empty + i, 4 * kMxSets);
     }
     *abort_flag = 0;
     mbar_fence_init();
   }
-  if (warp == 4) {
+  if (warp == kMxProducer) {
     prefetch_tensormap(&tm_x);
     prefetch_tensormap(&tm_w);
     prefetch_tensormap(&tm_y);
   }
-  if (warp == 5) {
+  if (warp == kMxIssuer) {
     tmem_alloc(tmem_slot, T::kTmem);
     tmem_relinquish();
   }
@@ -211,7 +242,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
 
   const int tiles = p.m_tiles * p.n_tiles;
   const int stages = (p.steps + 3) >> 2;
-  if (warp == 4) {
+  if (warp == kMxProducer) {
     // ---------------------------------------------------------------- producer
     const uint32_t a0 = smem_u32(ring_a), b0 = smem_u32(ring_b), s0 = smem_u32(ring_s), full0 = smem_u32(full), empty0 = smem_u32(empty);
     uint32_t s = 0, phase = 0;
@@ -240,7 +271,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
         }
       }
     }
-  } else if (warp == 5) {
+  } else if (warp == kMxIssuer) {
     // ---------------------------------------------------------------- MMA issuer
     const uint32_t a0 = desc_lo(smem_u32(ring_a)), b0 = desc_lo(smem_u32(ring_b)), s0 = desc_lo(smem_u32(ring_s));
     const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
@@ -283,21 +314,25 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
   } else {
     // ---------------------------------------------------------------- epilogue
     // (after a wait that ran out the warps go on through the barriers that they share, and touch nothing else)
-    const int row = threadIdx.x;
-    uint32_t buf = 0, acc_phase = 0, pieces = 0;
+    const int set = warp >> 2, row = threadIdx.x & 127;
+    uint8_t* out = staged + set * kMxStoreBytes;
+    uint32_t buf = 0, acc_phase = 0;
+    int turn = 0;  // the set that takes the next piece
     bool ok = true;
     for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
       const int m = t / p.n_tiles, n = t - m * p.n_tiles;
       ok = mbar_wait_warp(acc_full + buf, acc_phase, abort_flag, kMxWaitLimit) && ok;
       tc_fence_after();
-      const uint32_t acc = tmem + buf * BN + ((uint32_t)(warp * 32) << 16);
+      const uint32_t acc = tmem + buf * BN + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll 1
       for (int g = 0; g < BN / 64; ++g) {
         const int c0 = n * BN + 64 * g;
         if (c0 >= p.C_out) break;
-        if (threadIdx.x == 0) bulk_wait_group_read1();  // the buffer of the piece before the last one is free
-        epilogue_barrier();
-        uint8_t* out = staged + (pieces & 1) * kMxStoreBytes;
+        const bool mine = turn == set;
+        turn = turn + 1 == kMxSets ? 0 : turn + 1;
+        if (!mine) continue;
+        if (row == 0) bulk_wait_group_read0();  // the set's last piece has left its buffer
+        set_barrier(set);
         if (ok) {
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
@@ -322,12 +357,11 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
           }
           fence_proxy_async_smem();
         }
-        epilogue_barrier();
-        if (threadIdx.x == 0 && ok) {
+        set_barrier(set);
+        if (row == 0 && ok) {
           tma_store_2d(&tm_y, out, c0, m * 128);
           bulk_commit_group();
         }
-        ++pieces;
       }
       tc_fence_before();
       __syncwarp();
@@ -335,7 +369,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
       buf ^= 1u;
       if (buf == 0) acc_phase ^= 1u;
     }
-    if (threadIdx.x == 0) bulk_wait_group_read0();
+    if (row == 0) bulk_wait_group_read0();
   }
 
   tc_fence_before();
@@ -347,7 +381,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
     if (threadIdx.x == 0 && p.dev_status != nullptr) atomicExch(p.dev_status, (int)SSCONV_ERR_TIMEOUT);
     __syncthreads();
   }
-  if (warp == 5) {
+  if (warp == kMxIssuer) {
     tc_fence_after();
     tmem_dealloc(tmem, T::kTmem);
   }
@@ -390,18 +424,16 @@ MxKernel mx_kernel(int act, int* smem) {
 
 cudaError_t launch_quantize_mxfp4(const void* x, int64_t rows, int C, void* codes, void* scales, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
-  const uint32_t items = (uint32_t)(g.row_tiles * 128 * g.chunks);
   count_launch();
-  return launch_dependent(quantize_mxfp4_kernel, (items + 15u) / 16u, 256, st, (const uint4*)x, (uint32_t*)codes, (uint32_t*)scales, (uint32_t)rows,
-                          items, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
+  return launch_dependent(quantize_mxfp4_kernel, (unsigned)(g.row_tiles * g.chunks), 256, st, (const uint4*)x, (uint32_t*)codes, (uint4*)scales,
+                          (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
 cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int C, void* x, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
-  const uint64_t pieces = (uint64_t)rows * (C / 8);
   count_launch();
-  return launch_dependent(dequantize_mxfp4_kernel, (unsigned)((pieces + 255) / 256), 256, st, (const uint32_t*)codes, (const uint8_t*)scales, (uint4*)x,
-                          pieces, (uint32_t)(C / 8), (uint32_t)g.chunks, (uint32_t)g.blocks);
+  return launch_dependent(dequantize_mxfp4_kernel, (unsigned)(g.row_tiles * g.chunks), 256, st, (const uint32_t*)codes, (const uint8_t*)scales,
+                          (uint4*)x, (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
 int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales,

@@ -20,28 +20,53 @@ namespace ssconv {
 
 namespace {
 
-__device__ __forceinline__ void unpack8(const uint4& a, float (&v)[8]) {
+// Eight values are four pairs: most of the arithmetic works on two values at once.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ Pair both(float v) { return f32x2(v, v); }
+__device__ __forceinline__ float sum_of(Pair v) {
+  float lo, hi;
+  split2(v, lo, hi);
+  return lo + hi;
+}
+__device__ __forceinline__ void unpack8(const uint4& a, Pair (&v)[4]) {
   const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    v[2 * j] = bf16_lo(w[j]);
-    v[2 * j + 1] = bf16_hi(w[j]);
-  }
+  for (int j = 0; j < 4; ++j) v[j] = f32x2(bf16_lo(w[j]), bf16_hi(w[j]));
 }
-__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
-  return make_uint4(pack_bf16x2<false>(v[0], v[1]), pack_bf16x2<false>(v[2], v[3]), pack_bf16x2<false>(v[4], v[5]),
-                    pack_bf16x2<false>(v[6], v[7]));
+__device__ __forceinline__ uint32_t pack2(Pair v) {
+  float lo, hi;
+  split2(v, lo, hi);
+  return pack_bf16x2<false>(lo, hi);
 }
+__device__ __forceinline__ uint4 pack8(const Pair (&v)[4]) { return make_uint4(pack2(v[0]), pack2(v[1]), pack2(v[2]), pack2(v[3])); }
 // 8 of a vector of parameters, `otherwise` where there is none.
-__device__ __forceinline__ void params8(const float* p, int piece, bool live, float otherwise, float (&v)[8]) {
+__device__ __forceinline__ void params8(const float* p, int piece, bool live, float otherwise, Pair (&v)[4]) {
   if (p == nullptr || !live) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = otherwise;
+    for (int j = 0; j < 4; ++j) v[j] = both(otherwise);
     return;
   }
-  const float4 a = reinterpret_cast<const float4*>(p)[2 * piece], b = reinterpret_cast<const float4*>(p)[2 * piece + 1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  const ulonglong2 a = reinterpret_cast<const ulonglong2*>(p)[2 * piece], b = reinterpret_cast<const ulonglong2*>(p)[2 * piece + 1];
+  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
+__device__ __forceinline__ void store_pairs(float* p, int piece, const Pair (&v)[4]) {
+  reinterpret_cast<ulonglong2*>(p)[2 * piece] = make_ulonglong2(v[0], v[1]);
+  reinterpret_cast<ulonglong2*>(p)[2 * piece + 1] = make_ulonglong2(v[2], v[3]);
 }
 
 // Sums over a team's threads, known to all of them afterwards.  Teams of several warps are whole blocks; their sums alternate
@@ -91,30 +116,33 @@ struct TeamSum {
 
 // Mean (0 for RMS) and 1 / deviation of a row; two passes over the registers, so that a mean far from zero costs no digits.
 template <int V, bool BLOCK>
-__device__ __forceinline__ void row_statistics(const float (&v)[V][8], const bool (&live)[V], bool layer, float inv_c, float eps,
+__device__ __forceinline__ void row_statistics(const Pair (&v)[V][4], const bool (&live)[V], bool layer, float inv_c, float eps,
                                                TeamSum<BLOCK>& sum, float& mean, float& rstd) {
   mean = 0.0f;
   if (layer) {
-    float s = 0.0f;
+    Pair s = 0;
 #pragma unroll
     for (int k = 0; k < V; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s += v[k][j];  // (zeros in pieces past the row)
-    sum(s);
-    mean = s * inv_c;
+      for (int j = 0; j < 4; ++j) s = add2(s, v[k][j]);  // (zeros in pieces past the row)
+    float t = sum_of(s);
+    sum(t);
+    mean = t * inv_c;
   }
-  float q = 0.0f;
+  Pair q = 0;
+  const Pair less = both(-mean);
 #pragma unroll
   for (int k = 0; k < V; ++k)
     if (live[k]) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float d = v[k][j] - mean;
-        q = fmaf(d, d, q);
+      for (int j = 0; j < 4; ++j) {
+        const Pair d = add2(v[k][j], less);
+        q = fma2(d, d, q);
       }
     }
-  sum(q);
-  rstd = rsqrtf(q * inv_c + eps);
+  float t = sum_of(q);
+  sum(t);
+  rstd = rsqrtf(t * inv_c + eps);
 }
 
 struct ForwardParams {
@@ -156,7 +184,7 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_kernel(const Forwar
   }
   for (; row - ahead < p.rows; row += step) {
     const bool there = row < p.rows;
-    float bv[V][8], hv[V][8];
+    Pair bv[V][4], hv[V][4];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       unpack8(bn[k], bv[k]);
@@ -178,17 +206,17 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_kernel(const Forwar
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const int piece = sub + k * lanes;
-      float g[8];
+      Pair g[4];
       params8(gate, piece, own[k], 1.0f, g);
       if (POST) {
-        float a[8], c[8];
+        Pair a[4], c[4];
         params8(p.t.post_gamma, piece, own[k], 1.0f, a);
         params8(p.t.post_beta, piece, own[k], 0.0f, c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) bv[k][j] = fmaf((bv[k][j] - stats.x) * stats.y, a[j], c[j]);
+        for (int j = 0; j < 4; ++j) bv[k][j] = fma2(mul2(add2(bv[k][j], both(-stats.x)), both(stats.y)), a[j], c[j]);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) hv[k][j] = own[k] ? fmaf(g[j], bv[k][j], p.scale * hv[k][j]) : 0.0f;
+      for (int j = 0; j < 4; ++j) hv[k][j] = own[k] ? fma2(g[j], bv[k][j], mul2(both(p.scale), hv[k][j])) : 0ull;
       if (there && own[k] && h != nullptr) h[(int64_t)row * p.C8 + piece] = pack8(hv[k]);
     }
     if (PRE) {
@@ -196,11 +224,11 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_kernel(const Forwar
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const int piece = sub + k * lanes;
-        float a[8], c[8];
+        Pair a[4], c[4];
         params8(p.t.pre_gamma, piece, own[k], 1.0f, a);
         params8(p.t.pre_beta, piece, own[k], 0.0f, c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) hv[k][j] = fmaf((hv[k][j] - stats.z) * stats.w, a[j], c[j]);
+        for (int j = 0; j < 4; ++j) hv[k][j] = fma2(mul2(add2(hv[k][j], both(-stats.z)), both(stats.w)), a[j], c[j]);
         if (there && own[k]) y[(int64_t)row * p.C8 + piece] = pack8(hv[k]);
       }
     }
@@ -235,6 +263,13 @@ struct BackwardParams {
   float* unit_sums;           // [units][C]
 };
 
+// A row as it was loaded.
+template <int V>
+struct RawRow {
+  uint4 x[V], b[V], dh[V], dy[V];
+  float4 stats;
+};
+
 template <int V, bool BLOCK, bool POST, bool PRE>
 __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(const BackwardParams p) {
   extern __shared__ float rows_of_warps[];  // [warps][C], of warp crews
@@ -244,7 +279,6 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
   const int sub = BLOCK ? threadIdx.x : threadIdx.x & (lanes - 1);
   const int teams = BLOCK ? 1 : 32 / lanes, team = BLOCK ? 0 : (threadIdx.x & 31) / lanes;
   const int crews_per_block = BLOCK ? 1 : blockDim.x >> 5;
-  const int crew = blockIdx.x * crews_per_block + (BLOCK ? 0 : threadIdx.x >> 5);
   const int crews = gridDim.x * crews_per_block;
   const int C = 8 * p.C8;
   const float inv_c = 1.0f / (float)C;
@@ -258,148 +292,169 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
   bool own[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) own[k] = sub + k * lanes < p.C8;
-  float acc[kSums][V][8];
+  Pair acc[kSums][V][4];
 #pragma unroll
   for (int a = 0; a < kSums; ++a)
 #pragma unroll
     for (int k = 0; k < V; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[a][k][j] = 0.0f;
-  grid_dependency_wait();
+      for (int j = 0; j < 4; ++j) acc[a][k][j] = 0;
 
-  for (int u = crew; u < p.units; u += crews) {
-    const int image = u / p.units_per_gate;
-    const int64_t image_end = min((int64_t)p.rows, (int64_t)(image + 1) * p.gate_rows);
-    const int64_t first = (int64_t)image * p.gate_rows + (int64_t)(u - image * p.units_per_gate) * p.unit_rows;
-    const int64_t end = min(image_end, first + p.unit_rows);
-    const float* gate = p.t.gate;
-    if (gate != nullptr && p.image_gates) gate += (int64_t)image * C;
-    for (int64_t r0 = first; r0 < end; r0 += teams) {
-      const int64_t row = r0 + team;
-      const bool there = row < end;
-      float4 stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if ((POST || PRE) && there) stats = reinterpret_cast<const float4*>(p.t.stats)[row];
-      uint4 xr[V], br[V], hr[V], yr[V];
+  // A place among a crew's rows: a unit, the first of the teams' rows in it, and the unit's end.
+  struct Place {
+    int unit, image, row, end;
+  };
+  const auto start_of = [&](int unit) {
+    const int image = unit / p.units_per_gate;
+    const int first = image * p.gate_rows + (unit - image * p.units_per_gate) * p.unit_rows;
+    return Place{unit, image, first, (int)min((long long)p.rows, min((long long)(image + 1) * p.gate_rows, (long long)first + p.unit_rows))};
+  };
+  const auto load = [&](const Place& at, RawRow<V>& raw) {
+    const int row = at.row + team;
+    const bool there = at.unit < p.units && row < at.end;
+    if ((POST || PRE) && there) raw.stats = reinterpret_cast<const float4*>(p.t.stats)[row];
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        xr[k] = br[k] = hr[k] = yr[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (there && own[k]) {
-          const int64_t at = row * p.C8 + sub + k * lanes;
-          br[k] = b[at];
-          if (PRE) {
-            xr[k] = x[at];
-            yr[k] = dy[at];
-          }
-          if (dh != nullptr) hr[k] = dh[at];
-        }
-      }
-      float d[V][8], hat[V][8], pv[V][8];  // pv: bhat with a first norm, else b itself
-      float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const int piece = sub + k * lanes;
-        unpack8(br[k], pv[k]);
-        unpack8(hr[k], d[k]);
-        if (POST) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) pv[k][j] = (pv[k][j] - stats.x) * stats.y;
-        }
+    for (int k = 0; k < V; ++k) {
+      raw.x[k] = raw.b[k] = raw.dh[k] = raw.dy[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (there && own[k]) {
+        const int64_t i = (int64_t)row * p.C8 + sub + k * lanes;
+        raw.b[k] = b[i];
         if (PRE) {
-          float gv[8], a[8], c[8], g[8];
-          unpack8(xr[k], hat[k]);
-          unpack8(yr[k], gv);
-          params8(gate, piece, own[k], 1.0f, g);
-          params8(p.t.post_gamma, piece, POST && own[k], 1.0f, a);
-          params8(p.t.post_beta, piece, POST && own[k], 0.0f, c);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float pj = POST ? fmaf(pv[k][j], a[j], c[j]) : pv[k][j];
-            hat[k][j] = (fmaf(g[j], pj, p.scale * hat[k][j]) - stats.z) * stats.w;
-            acc[kPreGamma][k][j] = fmaf(gv[j], hat[k][j], acc[kPreGamma][k][j]);
-            acc[kPreBeta][k][j] += gv[j];
-          }
-          params8(p.t.pre_gamma, piece, own[k], 1.0f, a);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float q = gv[j] * a[j];
-            s1 += q;
-            s2 = fmaf(q, hat[k][j], s2);
-          }
+          raw.x[k] = x[i];
+          raw.dy[k] = dy[i];
         }
-      }
-      if (PRE) {
-        sum(s1, s2);
-        s1 = p.pre_layer ? s1 * inv_c : 0.0f;
-        s2 *= inv_c;
-      }
-      float t1 = 0.0f, t2 = 0.0f;
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const int piece = sub + k * lanes;
-        float a[8], c[8], g[8];
-        if (PRE) {
-          float gv[8];
-          unpack8(yr[k], gv);
-          params8(p.t.pre_gamma, piece, own[k], 1.0f, a);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) d[k][j] += stats.w * (gv[j] * a[j] - s1 - hat[k][j] * s2);
-        }
-        if (there && own[k] && dx != nullptr) {
-          float o[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] = p.scale * d[k][j];
-          dx[row * p.C8 + piece] = pack8(o);
-        }
-        params8(gate, piece, own[k], 1.0f, g);
-        params8(p.t.post_gamma, piece, POST && own[k], 1.0f, a);
-        params8(p.t.post_beta, piece, POST && own[k], 0.0f, c);
-        if (there && own[k]) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float pj = POST ? fmaf(pv[k][j], a[j], c[j]) : pv[k][j];
-            acc[kGate][k][j] = fmaf(d[k][j], pj, acc[kGate][k][j]);
-            d[k][j] *= g[j];  // dp from here on
-            if (POST) {
-              acc[kPostGamma][k][j] = fmaf(d[k][j], pv[k][j], acc[kPostGamma][k][j]);
-              acc[kPostBeta][k][j] += d[k][j];
-              d[k][j] *= a[j];
-              t1 += d[k][j];
-              t2 = fmaf(d[k][j], pv[k][j], t2);
-            }
-          }
-        }
-      }
-      if (POST) {
-        sum(t1, t2);
-        t1 = p.post_layer ? t1 * inv_c : 0.0f;
-        t2 *= inv_c;
-      }
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        if (POST) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) d[k][j] = stats.y * (d[k][j] - t1 - pv[k][j] * t2);
-        }
-        if (there && own[k] && db != nullptr) db[row * p.C8 + sub + k * lanes] = pack8(d[k]);
+        if (dh != nullptr) raw.dh[k] = dh[i];
       }
     }
-    if (p.image_gates && p.g.dgate != nullptr) {
-      float* out = p.units_per_gate == 1 ? p.g.dgate + (int64_t)image * C : p.unit_sums + (int64_t)u * C;
+  };
+
+  grid_dependency_wait();
+  Place at = start_of(blockIdx.x * crews_per_block + (BLOCK ? 0 : threadIdx.x >> 5));
+  RawRow<V> coming;
+  coming.stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  load(at, coming);
+  while (at.unit < p.units) {
+    const RawRow<V> raw = coming;
+    Place next = at;
+    next.row += teams;
+    if (next.row >= at.end) next = start_of(at.unit + crews);
+    load(next, coming);
+    const int row = at.row + team;
+    const bool there = row < at.end;
+    const float* gate = p.t.gate;
+    if (gate != nullptr && p.image_gates) gate += (int64_t)at.image * C;
+
+    Pair d[V][4], hat[V][4], pv[V][4];  // pv: bhat with a first norm, else b itself
+    Pair s1 = 0, s2 = 0;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int piece = sub + k * lanes;
+      unpack8(raw.b[k], pv[k]);
+      unpack8(raw.dh[k], d[k]);
+      if (POST) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pv[k][j] = mul2(add2(pv[k][j], both(-raw.stats.x)), both(raw.stats.y));
+      }
+      if (PRE) {
+        Pair gv[4], a[4], c[4], g[4];
+        unpack8(raw.x[k], hat[k]);
+        unpack8(raw.dy[k], gv);
+        params8(gate, piece, own[k], 1.0f, g);
+        if (POST) {
+          params8(p.t.post_gamma, piece, own[k], 1.0f, a);
+          params8(p.t.post_beta, piece, own[k], 0.0f, c);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const Pair pj = POST ? fma2(pv[k][j], a[j], c[j]) : pv[k][j];
+          const Pair h = fma2(g[j], pj, mul2(both(p.scale), hat[k][j]));
+          hat[k][j] = mul2(add2(h, both(-raw.stats.z)), both(raw.stats.w));
+          acc[kPreGamma][k][j] = fma2(gv[j], hat[k][j], acc[kPreGamma][k][j]);
+          acc[kPreBeta][k][j] = add2(acc[kPreBeta][k][j], gv[j]);
+        }
+        params8(p.t.pre_gamma, piece, own[k], 1.0f, a);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const Pair q = mul2(gv[j], a[j]);
+          s1 = add2(s1, q);
+          s2 = fma2(q, hat[k][j], s2);
+          // dh plus what the norm hands back, but for the means
+          d[k][j] = fma2(q, both(raw.stats.w), d[k][j]);
+        }
+      }
+    }
+    Pair from_mean = 0, from_hat = 0;
+    if (PRE) {
+      float m = sum_of(s1), q = sum_of(s2);
+      sum(m, q);
+      from_mean = both(p.pre_layer ? -raw.stats.w * (m * inv_c) : 0.0f);
+      from_hat = both(-raw.stats.w * (q * inv_c));
+    }
+    Pair t1 = 0, t2 = 0;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int piece = sub + k * lanes;
+      Pair a[4], c[4], g[4];
+      if (PRE) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[k][j] = add2(fma2(hat[k][j], from_hat, from_mean), d[k][j]);
+      }
+      if (there && own[k] && dx != nullptr) {
+        Pair o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = mul2(both(p.scale), d[k][j]);
+        dx[(int64_t)row * p.C8 + piece] = pack8(o);
+      }
+      params8(gate, piece, own[k], 1.0f, g);
+      if (POST) {
+        params8(p.t.post_gamma, piece, own[k], 1.0f, a);
+        params8(p.t.post_beta, piece, own[k], 0.0f, c);
+      }
+      if (there && own[k]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const Pair pj = POST ? fma2(pv[k][j], a[j], c[j]) : pv[k][j];
+          acc[kGate][k][j] = fma2(d[k][j], pj, acc[kGate][k][j]);
+          d[k][j] = mul2(d[k][j], g[j]);  // dp from here on
+          if (POST) {
+            acc[kPostGamma][k][j] = fma2(d[k][j], pv[k][j], acc[kPostGamma][k][j]);
+            acc[kPostBeta][k][j] = add2(acc[kPostBeta][k][j], d[k][j]);
+            d[k][j] = mul2(d[k][j], a[j]);
+            t1 = add2(t1, d[k][j]);
+            t2 = fma2(d[k][j], pv[k][j], t2);
+          }
+        }
+      }
+    }
+    if (POST) {
+      float m = sum_of(t1), q = sum_of(t2);
+      sum(m, q);
+      from_mean = both(p.post_layer ? -raw.stats.y * (m * inv_c) : 0.0f);
+      from_hat = both(-raw.stats.y * (q * inv_c));
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      if (POST) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[k][j] = fma2(d[k][j], both(raw.stats.y), fma2(pv[k][j], from_hat, from_mean));
+      }
+      if (there && own[k] && db != nullptr) db[(int64_t)row * p.C8 + sub + k * lanes] = pack8(d[k]);
+    }
+
+    if (next.unit != at.unit && p.image_gates && p.g.dgate != nullptr) {
+      float* out = p.units_per_gate == 1 ? p.g.dgate + (int64_t)at.image * C : p.unit_sums + (int64_t)at.unit * C;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         if (!BLOCK)
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            for (int o = 16; o >= lanes; o >>= 1) acc[kGate][k][j] += __shfl_xor_sync(0xFFFFFFFFu, acc[kGate][k][j], o);
-        if (own[k] && team == 0) {
-          float4* w = reinterpret_cast<float4*>(out) + 2 * (sub + k * lanes);
-          w[0] = make_float4(acc[kGate][k][0], acc[kGate][k][1], acc[kGate][k][2], acc[kGate][k][3]);
-          w[1] = make_float4(acc[kGate][k][4], acc[kGate][k][5], acc[kGate][k][6], acc[kGate][k][7]);
-        }
+          for (int j = 0; j < 4; ++j)
+            for (int o = 16; o >= lanes; o >>= 1) acc[kGate][k][j] = add2(acc[kGate][k][j], __shfl_xor_sync(0xFFFFFFFFu, acc[kGate][k][j], o));
+        if (own[k] && team == 0) store_pairs(out, sub + k * lanes, acc[kGate][k]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[kGate][k][j] = 0.0f;
+        for (int j = 0; j < 4; ++j) acc[kGate][k][j] = 0;
       }
     }
+    at = next;
   }
 
   // What is left in the registers, summed over the block's warps and teams.
@@ -416,13 +471,9 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
     for (int k = 0; k < V; ++k) {
       if (!BLOCK)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          for (int o = 16; o >= lanes; o >>= 1) acc[a][k][j] += __shfl_xor_sync(0xFFFFFFFFu, acc[a][k][j], o);
-      if (own[k] && team == 0) {
-        float4* w = reinterpret_cast<float4*>(out) + 2 * (sub + k * lanes);
-        w[0] = make_float4(acc[a][k][0], acc[a][k][1], acc[a][k][2], acc[a][k][3]);
-        w[1] = make_float4(acc[a][k][4], acc[a][k][5], acc[a][k][6], acc[a][k][7]);
-      }
+        for (int j = 0; j < 4; ++j)
+          for (int o = 16; o >= lanes; o >>= 1) acc[a][k][j] = add2(acc[a][k][j], __shfl_xor_sync(0xFFFFFFFFu, acc[a][k][j], o));
+      if (own[k] && team == 0) store_pairs(out, sub + k * lanes, acc[a][k]);
     }
     if (!BLOCK) {
       __syncthreads();
@@ -439,49 +490,51 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
 struct FinishParams {
   const float* block_sums;
   const float* unit_sums;
-  float* out[kSums];          // (nullptr: not wanted)
-  int blocks, C;
+  float* out[kSums];          // the sums that are wanted ...
+  int kind[kSums];            // ... and where they are among a block's
+  int wanted, blocks, C;
   int images, units_per_gate; // of gates per image whose units were several (0 images: none)
   float* dgate;
 };
-// 32 columns x 32 rows of threads: column sums of one kind over the blocks, or of one image's units.
+// First the sums over blocks, 32 columns x 32 rows of threads; then those of the images' units, 4 columns per thread.
 __global__ void __launch_bounds__(1024) resnorm_finish_kernel(const FinishParams p) {
   __shared__ float part[32][33];
   grid_launch_dependents();
   grid_dependency_wait();
   const int groups = (p.C + 31) / 32;
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int col = (blockIdx.x % groups) * 32 + tx;
-  const int job = blockIdx.x / groups;
-  const float* in;
-  float* out;
-  int n;
-  int64_t pitch;
-  if (job < kSums) {
-    in = p.block_sums + (int64_t)job * p.C;
-    out = p.out[job];
-    n = p.blocks;
-    pitch = (int64_t)kSums * p.C;
-  } else {
-    const int image = job - kSums;
-    in = p.unit_sums + (int64_t)image * p.units_per_gate * p.C;
-    out = p.dgate + (int64_t)image * p.C;
-    n = p.units_per_gate;
-    pitch = p.C;
-  }
-  if (out == nullptr) return;
-  float s = 0.0f;
-  if (col < p.C) {
-#pragma unroll 4
-    for (int r = ty; r < n; r += 32) s += in[r * pitch + col];
-  }
-  part[ty][tx] = s;
-  __syncthreads();
-  s = part[tx][ty];  // column ty of the group, row tx of the partial sums
+  int job = blockIdx.x;
+  if (job < groups * p.wanted) {
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int which = job / groups, col = (job - which * groups) * 32 + tx;
+    const float* in = p.block_sums + (int64_t)p.kind[which] * p.C + col;
+    const int64_t pitch = (int64_t)kSums * p.C;
+    float s = 0.0f;
+    if (col < p.C) {
+#pragma unroll 8
+      for (int r = ty; r < p.blocks; r += 32) s += in[r * pitch];
+    }
+    part[ty][tx] = s;
+    __syncthreads();
+    s = part[tx][ty];  // column ty of the group, row tx of the partial sums
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xFFFFFFFFu, s, o);
-  const int c = (blockIdx.x % groups) * 32 + ty;
-  if (tx == 0 && c < p.C) out[c] = s;
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xFFFFFFFFu, s, o);
+    const int c = col - tx + ty;
+    if (tx == 0 && c < p.C) p.out[which][c] = s;
+    return;
+  }
+  job -= groups * p.wanted;
+  const int64_t i = (int64_t)job * 1024 + threadIdx.x;
+  const int C4 = p.C / 4;
+  if (i >= (int64_t)p.images * C4) return;
+  const int64_t image = i / C4;
+  const float4* in = reinterpret_cast<const float4*>(p.unit_sums) + image * p.units_per_gate * C4 + (i - image * C4);
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int u = 0; u < p.units_per_gate; ++u) {
+    const float4 v = in[(int64_t)u * C4];
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  reinterpret_cast<float4*>(p.dgate)[i] = s;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -525,7 +578,7 @@ struct Cut {
   int units, unit_rows, units_per_gate, gate_rows, blocks, images;
   bool image_gates;
 };
-constexpr int kBackwardWarps = 16;       // per SM, of crews at work at once
+constexpr int kBackwardWarps = 16;       // per SM, of crews at work at once (half as many with two pieces per lane of a warp)
 constexpr int kRowsPerTeam = 4;          // of a unit, at least: its sums are written once
 
 Cut cut_backward(const ssconv_resnorm_t& d) {
@@ -538,12 +591,25 @@ Cut cut_backward(const ssconv_resnorm_t& d) {
   const int crew_warps = c.team.block ? c.team.threads / 32 : 1;
   const int teams = c.team.block ? 1 : 32 / c.team.lanes;
   const int crews_per_block = c.team.block ? 1 : c.team.threads / 32;
-  const int64_t most = (int64_t)device_sms() * (kBackwardWarps / crew_warps > 0 ? kBackwardWarps / crew_warps : 1);
-  int64_t per_gate = (most + c.images - 1) / c.images;
+  const int warps = !c.team.block && c.team.V == 2 ? kBackwardWarps / 2 : kBackwardWarps;
+  const int64_t most = (int64_t)device_sms() * (warps / crew_warps > 0 ? warps / crew_warps : 1);
+  // Units per row of gates: as many as keep the crew with the most rows short, fewer where it makes no difference.
   const int64_t worth = (c.gate_rows + teams * kRowsPerTeam - 1) / (teams * kRowsPerTeam);
-  if (per_gate > worth) per_gate = worth;
-  c.unit_rows = (int)((c.gate_rows + per_gate - 1) / per_gate);
-  c.units_per_gate = (c.gate_rows + c.unit_rows - 1) / c.unit_rows;
+  const int64_t all = most / c.images < 1 ? 1 : most / c.images;
+  int64_t least = -1;
+  for (int64_t k = 1; k <= 9; ++k) {
+    int64_t units = k == 9 ? all : k;
+    if (units > worth) units = worth;
+    const int64_t unit_rows = (c.gate_rows + units - 1) / units;
+    units = (c.gate_rows + unit_rows - 1) / unit_rows;
+    const int64_t turns = (c.images * units + most - 1) / most;
+    const int64_t cost = turns * ((unit_rows + teams - 1) / teams + 1);
+    if (least < 0 || cost < least) {
+      least = cost;
+      c.unit_rows = (int)unit_rows;
+      c.units_per_gate = (int)units;
+    }
+  }
   c.units = c.images * c.units_per_gate;
   const int64_t crews = c.units < most ? c.units : most;
   c.blocks = (int)((crews + crews_per_block - 1) / crews_per_block);
@@ -605,19 +671,20 @@ cudaError_t launch_resnorm_backward(const ssconv_resnorm_t& d, const ResnormTens
   FinishParams f = {};
   f.block_sums = p.block_sums;
   f.unit_sums = p.unit_sums;
-  bool any = false;
-  for (int i = 0; i < kSums; ++i) {
-    f.out[i] = i == kGate && c.image_gates ? nullptr : sums[i];
-    any = any || f.out[i] != nullptr;
-  }
+  for (int i = 0; i < kSums; ++i)
+    if (sums[i] != nullptr && !(i == kGate && c.image_gates)) {
+      f.out[f.wanted] = sums[i];
+      f.kind[f.wanted++] = i;
+    }
   f.blocks = c.blocks;
   f.C = d.C;
   f.units_per_gate = c.units_per_gate;
   f.images = c.image_gates && c.units_per_gate > 1 && g.dgate != nullptr ? c.images : 0;
   f.dgate = g.dgate;
-  if (!any && f.images == 0) return cudaSuccess;
+  const int64_t blocks = (int64_t)((d.C + 31) / 32) * f.wanted + ((int64_t)f.images * (d.C / 4) + 1023) / 1024;
+  if (blocks == 0) return cudaSuccess;
   count_launch();
-  return launch_dependent(resnorm_finish_kernel, (unsigned)((d.C + 31) / 32 * (kSums + f.images)), 1024, st, f);
+  return launch_dependent(resnorm_finish_kernel, (unsigned)blocks, 1024, st, f);
 }
 
 }  // namespace ssconv

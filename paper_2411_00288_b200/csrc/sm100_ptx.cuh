@@ -135,6 +135,16 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return d;
 }
 
+// Two fp32 values in a register pair, for the instructions that work on both at once.
+__device__ __forceinline__ unsigned long long f32x2(float lo, float hi) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split2(unsigned long long v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+
 // Programmatic dependent launch: a grid launched with programmatic stream serialisation may start
 // while the grid before it in the stream is still running.  grid_dependency_wait() returns once
 // that grid has completed and its memory operations are visible; until then this grid must not
