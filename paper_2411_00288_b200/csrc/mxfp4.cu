@@ -20,15 +20,21 @@ namespace {
 // four lanes a block of 32, each thread eight rows: eight loads in flight, and the image is written whole.  DRAM-bound: 2.53
 // bytes per element.
 // ---------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, float scale) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// The larger of two pairs of magnitudes, a NaN where there is one.
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// (Scaled as bf16 pairs: a product by a power of two is exact, but for those so small that they round to zero anyway.)
+__device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, uint32_t scale_x2) {
+  const uint32_t w[4] = {mul_bf16x2(v.x, scale_x2), mul_bf16x2(v.y, scale_x2), mul_bf16x2(v.z, scale_x2), mul_bf16x2(v.w, scale_x2)};
   uint32_t out;
-  float f[8];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    f[2 * j] = bf16_lo(w[j]) * scale;
-    f[2 * j + 1] = bf16_hi(w[j]) * scale;
-  }
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
@@ -36,10 +42,10 @@ __device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, float scale) {
       "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
       "mov.b32 %0, {a, b, c, d};\n\t}"
       : "=r"(out)
-      : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
+      : "f"(bf16_lo(w[0])), "f"(bf16_hi(w[0])), "f"(bf16_lo(w[1])), "f"(bf16_hi(w[1])), "f"(bf16_lo(w[2])), "f"(bf16_hi(w[2])), "f"(bf16_lo(w[3])),
+        "f"(bf16_hi(w[3])));
   return out;
 }
-__device__ __forceinline__ uint32_t magnitude_bits(uint32_t pair) { return max(pair & 0x7FFFu, (pair >> 16) & 0x7FFFu); }
 
 constexpr int kMxRowsPerThread = 8;  // 16 rows of threads
 
@@ -62,12 +68,13 @@ __global__ void __launch_bounds__(256) quantize_mxfp4_kernel(const uint4* x, uin
 #pragma unroll
   for (int u = 0; u < kMxRowsPerThread; ++u) {
     const uint32_t r = r0 + 16u * u;
-    uint32_t m = max(max(magnitude_bits(v[u].x), magnitude_bits(v[u].y)), max(magnitude_bits(v[u].z), magnitude_bits(v[u].w)));
-    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-    const uint32_t e = m >> 7;
+    constexpr uint32_t kMagnitudes = 0x7FFF7FFFu;
+    uint32_t m = max_bf16x2(max_bf16x2(v[u].x & kMagnitudes, v[u].y & kMagnitudes), max_bf16x2(v[u].z & kMagnitudes, v[u].w & kMagnitudes));
+    m = max_bf16x2(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+    m = max_bf16x2(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+    const uint32_t e = max(m & 0xFFFFu, m >> 16) >> 7;
     const uint32_t code = e == 255u ? 255u : e < 2u ? 0u : e - 2u;
-    const float inverse = __uint_as_float((254u - min(code, 252u)) << 23);
+    const uint32_t inverse = ((254u - min(code, 252u)) << 7) * 0x10001u;
     if (r < there && (piece >> 2) < blocks) codes[(uint64_t)(tile * 128u + r) * (4u * blocks) + piece] = e2m1_x8(v[u], inverse);
     uint32_t word = code << (8u * (lane >> 2));
     word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
@@ -78,11 +85,13 @@ __global__ void __launch_bounds__(256) quantize_mxfp4_kernel(const uint4* x, uin
   if (threadIdx.x < 32) scales[(uint64_t)blockIdx.x * 32u + threadIdx.x] = reinterpret_cast<const uint4*>(image)[threadIdx.x];
 }
 
-// The values of codes: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, times the scale; exact in bf16.
-__device__ __forceinline__ float e2m1_value(uint32_t code) {
-  const uint32_t e = (code >> 1) & 3u, m = code & 1u;
-  const uint32_t bits = e ? ((e + 126u) << 23) | (m << 22) : m * 0x3F000000u;
-  return __uint_as_float(bits | ((code & 8u) << 28));
+// The bf16 values of four codes (the low 16 bits): their high and low bytes looked up by the three bits below the sign, the
+// bytes put together, the signs above.  0, 1/2, 1, 3/2, 2, 3, 4, 6 are 0, 3F00, 3F80, 3FC0, 4000, 4040, 4080, 40C0.
+__device__ __forceinline__ void e2m1_values_x4(uint32_t codes, uint32_t& low, uint32_t& high) {
+  const uint32_t select = codes & 0x7777u;
+  const uint32_t hi = __byte_perm(0x3F3F3F00u, 0x40404040u, select), lo = __byte_perm(0xC0800000u, 0xC0804000u, select);
+  low = __byte_perm(lo, hi, 0x5140) | ((codes << 12) & 0x8000u) | ((codes << 24) & 0x80000000u);
+  high = __byte_perm(lo, hi, 0x7362) | ((codes << 4) & 0x8000u) | ((codes << 16) & 0x80000000u);
 }
 __global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint32_t rows, uint32_t chunks,
                                                                uint32_t blocks, uint32_t C8) {
@@ -106,13 +115,14 @@ __global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* c
 #pragma unroll
   for (int u = 0; u < kMxRowsPerThread; ++u) {
     const uint32_t r = r0 + 16u * u;
-    const float scale = __uint_as_float(s[u] == 255u ? 0x7FC00000u : s[u] == 0u ? 0x00400000u : s[u] << 23);
-    float f[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = e2m1_value(c[u] >> (4 * j)) * scale;
+    // the scale as bf16: 2^-127 is below the normal numbers, 255 is a NaN
+    const uint32_t scale = (s[u] == 255u ? 0x7FC0u : s[u] == 0u ? 0x0040u : s[u] << 7) * 0x10001u;
+    uint4 o;
+    e2m1_values_x4(c[u] & 0xFFFFu, o.x, o.y);
+    e2m1_values_x4(c[u] >> 16, o.z, o.w);
     if (r < there)
       x[(uint64_t)(tile * 128u + r) * C8 + piece] =
-          make_uint4(pack_bf16x2<false>(f[0], f[1]), pack_bf16x2<false>(f[2], f[3]), pack_bf16x2<false>(f[4], f[5]), pack_bf16x2<false>(f[6], f[7]));
+          make_uint4(mul_bf16x2(o.x, scale), mul_bf16x2(o.y, scale), mul_bf16x2(o.z, scale), mul_bf16x2(o.w, scale));
   }
 }
 
@@ -121,25 +131,25 @@ __global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* c
 // K in stages of 256 channels (128 bytes of codes per row, the 128-byte swizzle; two scale images per 128 rows).  One thread block
 // per SM walks over tiles, channels first, so that the blocks at work at a time share few rows of x; two accumulators, so that a
 // tile's epilogue runs beside the next one's MMAs.  The epilogue's pieces (64 channels) go to kMxSets sets of four warps in turn;
-// two more warps are the producer and the MMA issuer.
+// each warp stages and stores its 32 rows by itself.  Two more warps are the producer and the MMA issuer.
 // ---------------------------------------------------------------------------------------
 constexpr long long kMxWaitLimit = 4000000000LL;  // cycles: about 2 s
+constexpr int kMxStoreBytes = 32 * 128;           // staged outputs of a warp: 32 pixels x 64 channels of bf16
 constexpr int kMxSets = 3;
-constexpr int kMxProducer = 4 * kMxSets, kMxIssuer = kMxProducer + 1;  // warps
-constexpr int kMxThreads = 32 * (kMxIssuer + 1);
-constexpr int kMxStoreBytes = 128 * 128;          // staged outputs: 128 pixels x 64 channels of bf16
 constexpr int kMxMostSmem = 227 * 1024;
 
 template <int BN>
 struct MxTile {
+  static constexpr int kProducer = 4 * kMxSets, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 1);
+  static constexpr int kStagedBytes = 4 * kMxSets * kMxStoreBytes;
   static constexpr int kScaleTiles = BN > 128 ? 2 : 1;  // images along the tile's channels
   static constexpr int kBytesA = 128 * 128, kBytesB = BN * 128, kBytesScales = 1024 * (1 + kScaleTiles);
   static constexpr int kBytes = kBytesA + kBytesB + kBytesScales;
-  static constexpr int kRoom = kMxMostSmem - 1024 - kMxSets * kMxStoreBytes - 256;
+  static constexpr int kRoom = kMxMostSmem - 1024 - kStagedBytes - 256;
   static constexpr int kStages = kRoom / kBytes < 6 ? kRoom / kBytes : 6;
   static constexpr int kScaleColumns = 8 * (1 + kScaleTiles);  // of TMEM, per stage: two images of x, two (four) of w
   static constexpr int kTmem = 2 * BN + kStages * kScaleColumns <= 256 ? 256 : 512;
-  static constexpr int kSmem = 1024 + kStages * kBytes + kMxSets * kMxStoreBytes + 256;
+  static constexpr int kSmem = 1024 + kStages * kBytes + kStagedBytes + 256;
   static_assert(2 * BN + kStages * kScaleColumns <= 512 && kStages >= 3, "");
 };
 
@@ -149,7 +159,13 @@ struct MxParams {
   int32_t* dev_status;
   int m_tiles, n_tiles, w_tiles;  // w_tiles: scale images along C_out
   int C_out, chunks, steps;       // steps of 64 channels
+  int tail_bytes;                 // of codes per row in the last stage's tiles: 32, 64 or 128
+  uint32_t tail_desc;             // high half of their descriptors
 };
+
+// High halves of descriptors of K-major tiles with rows of 64 and of 32 bytes in the swizzles of those widths.
+constexpr uint32_t kDescHiSw64 = (512u >> 4) | (1u << 14) | (4u << 29);
+constexpr uint32_t kDescHiSw32 = (256u >> 4) | (1u << 14) | (6u << 29);
 
 // 32x128b.warpx4: 512 bytes (32 rows of 16, unswizzled) into 4 TMEM columns, the same 32 lanes in each of the four quarters.
 __device__ __forceinline__ void tc_cp_32x128b_x4_w(uint32_t dst_tmem, uint32_t src_lo) {
@@ -162,8 +178,8 @@ __device__ __forceinline__ void tc_cp_32x128b_x4_w(uint32_t dst_tmem, uint32_t s
       : "memory");
 }
 // D[128 x N] (+)= A[128 x 64] B[N x 64]^T, e2m1 operands with one e8m0 scale per 32 elements of a row, taken from TMEM.
-__device__ __forceinline__ void tc_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                              uint32_t accumulate) {
+__device__ __forceinline__ void tc_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
+                                              uint32_t sfb, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
       "elect.sync _|e, 0xffffffff;\n\t"
@@ -171,7 +187,7 @@ __device__ __forceinline__ void tc_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, ui
       "mov.b64 db, {%2, %7};\n\t"
       "setp.ne.b32 p, %6, 0;\n\t"
       "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(kDescHiSw128)
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(desc_hi)
       : "memory");
 }
 // Instruction descriptor of kind::mxf4: bits 4-5 and 29-30 which of a row's scales in its TMEM word (0 or 2: the first two or the
@@ -180,24 +196,30 @@ __device__ __forceinline__ void tc_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, ui
 __host__ __device__ constexpr uint32_t make_idesc_mxf4(uint32_t N, uint32_t which) {
   return (which << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (1u << 23) | (1u << 27) | (which << 29);
 }
-// 32 columns of the warp's 32 lanes: register i of lane t holds column i of row t.
-__device__ __forceinline__ void tc_ld_32x32b_x32(uint32_t taddr, uint32_t (&r)[32]) {
+// 16 columns of the warp's 32 lanes: register i of lane t holds column i of row t, after the wait below.
+__device__ __forceinline__ void tc_ld_32x32b_x16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
-        "=r"(r[30]), "=r"(r[31])
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
 }
-// The four warps of a set.
-__device__ __forceinline__ void set_barrier(int set) { asm volatile("bar.sync %0, 128;" ::"r"(1 + set) : "memory"); }
+// (The registers go through the wait, so that nothing that uses them is moved before it.)
+__device__ __forceinline__ void tc_wait_ld_x16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
 
 template <int BN, int ACT>
-__global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
+__global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __grid_constant__ CUtensorMap tm_x,
+                                                             const __grid_constant__ CUtensorMap tm_w,
+                                                             const __grid_constant__ CUtensorMap tm_x_tail,
+                                                             const __grid_constant__ CUtensorMap tm_w_tail,
                                                              const __grid_constant__ CUtensorMap tm_y, const MxParams p) {
   using T = MxTile<BN>;
   extern __shared__ uint8_t smem_raw[];
@@ -205,7 +227,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
   uint8_t* ring_a = smem;
   uint8_t* ring_b = ring_a + T::kStages * T::kBytesA;
   uint8_t* staged = ring_b + T::kStages * T::kBytesB;
-  uint8_t* ring_s = staged + kMxSets * kMxStoreBytes;
+  uint8_t* ring_s = staged + T::kStagedBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring_s + T::kStages * T::kBytesScales);
   uint64_t *full = bars, *empty = bars + T::kStages, *acc_full = bars + 2 * T::kStages, *acc_empty = acc_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
@@ -225,12 +247,14 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
     *abort_flag = 0;
     mbar_fence_init();
   }
-  if (warp == kMxProducer) {
+  if (warp == T::kProducer) {
     prefetch_tensormap(&tm_x);
     prefetch_tensormap(&tm_w);
+    prefetch_tensormap(&tm_x_tail);
+    prefetch_tensormap(&tm_w_tail);
     prefetch_tensormap(&tm_y);
   }
-  if (warp == kMxIssuer) {
+  if (warp == T::kIssuer) {
     tmem_alloc(tmem_slot, T::kTmem);
     tmem_relinquish();
   }
@@ -242,7 +266,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
 
   const int tiles = p.m_tiles * p.n_tiles;
   const int stages = (p.steps + 3) >> 2;
-  if (warp == kMxProducer) {
+  if (warp == T::kProducer) {
     // ---------------------------------------------------------------- producer
     const uint32_t a0 = smem_u32(ring_a), b0 = smem_u32(ring_b), s0 = smem_u32(ring_s), full0 = smem_u32(full), empty0 = smem_u32(empty);
     uint32_t s = 0, phase = 0;
@@ -259,9 +283,10 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
         }
         const uint32_t bar = full0 + 8 * s, sc = s0 + s * T::kBytesScales;
         const uint32_t part = min(2, p.chunks - 2 * kb) * kMxImageBytes;
-        mbar_expect_tx_w(bar, T::kBytesA + T::kBytesB + part * (1 + images));
-        tma_load_2d_w(a0 + s * T::kBytesA, &tm_x, bar, kb * 128, m * 128);
-        tma_load_2d_w(b0 + s * T::kBytesB, &tm_w, bar, kb * 128, n * BN);
+        const bool tail = kb == stages - 1;
+        mbar_expect_tx_w(bar, (tail ? p.tail_bytes : 128) * (128 + BN) + part * (1 + images));
+        tma_load_2d_w(a0 + s * T::kBytesA, tail ? &tm_x_tail : &tm_x, bar, kb * 128, m * 128);
+        tma_load_2d_w(b0 + s * T::kBytesB, tail ? &tm_w_tail : &tm_w, bar, kb * 128, n * BN);
         bulk_load_w(sc, xs + kb * 2 * kMxImageBytes, part, bar);
         for (int i = 0; i < images; ++i)
           bulk_load_w(sc + 1024 * (1 + i), p.w_scales + ((int64_t)(first + i) * p.chunks + 2 * kb) * kMxImageBytes, part, bar);
@@ -271,7 +296,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
         }
       }
     }
-  } else if (warp == kMxIssuer) {
+  } else if (warp == T::kIssuer) {
     // ---------------------------------------------------------------- MMA issuer
     const uint32_t a0 = desc_lo(smem_u32(ring_a)), b0 = desc_lo(smem_u32(ring_b)), s0 = desc_lo(smem_u32(ring_s));
     const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
@@ -292,14 +317,15 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
         const uint32_t sfa = tmem + 2 * BN + s * T::kScaleColumns, sfb = sfa + 8;
         const uint32_t src = s0 + s * (T::kBytesScales >> 4);
         const int steps = min(4, p.steps - 4 * kb);
+        const uint32_t desc_hi = kb == stages - 1 ? p.tail_desc : kDescHiSw128;
         for (int c = 0; 2 * c < steps; ++c) {
           tc_cp_32x128b_x4_w(sfa + 4 * c, src + 32 * c);
 #pragma unroll
           for (int i = 0; i < T::kScaleTiles; ++i) tc_cp_32x128b_x4_w(sfb + 4 * T::kScaleTiles * c + 4 * i, src + 64 * (1 + i) + 32 * c);
         }
         for (int k = 0; k < steps; ++k)
-          tc_mma_mxf4_w(d, a0 + s * (T::kBytesA >> 4) + 2 * k, b0 + s * (T::kBytesB >> 4) + 2 * k, make_idesc_mxf4(BN, 2 * (k & 1)),
-                        sfa + 4 * (k >> 1), sfb + 4 * T::kScaleTiles * (k >> 1) + shift, (kb | k) != 0);
+          tc_mma_mxf4_w(d, a0 + s * (T::kBytesA >> 4) + 2 * k, b0 + s * (T::kBytesB >> 4) + 2 * k, desc_hi,
+                        make_idesc_mxf4(BN, 2 * (k & 1)), sfa + 4 * (k >> 1), sfb + 4 * T::kScaleTiles * (k >> 1) + shift, (kb | k) != 0);
         tc_commit_w(empty0 + 8 * s);
         if (++s == T::kStages) {
           s = 0;
@@ -313,17 +339,15 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
     }
   } else {
     // ---------------------------------------------------------------- epilogue
-    // (after a wait that ran out the warps go on through the barriers that they share, and touch nothing else)
-    const int set = warp >> 2, row = threadIdx.x & 127;
-    uint8_t* out = staged + set * kMxStoreBytes;
+    const int set = warp >> 2, row = 32 * (warp & 3), lane = threadIdx.x & 31;
+    uint8_t* out = staged + warp * kMxStoreBytes;
     uint32_t buf = 0, acc_phase = 0;
     int turn = 0;  // the set that takes the next piece
-    bool ok = true;
     for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
       const int m = t / p.n_tiles, n = t - m * p.n_tiles;
-      ok = mbar_wait_warp(acc_full + buf, acc_phase, abort_flag, kMxWaitLimit) && ok;
+      if (!mbar_wait_warp(acc_full + buf, acc_phase, abort_flag, kMxWaitLimit)) break;
       tc_fence_after();
-      const uint32_t acc = tmem + buf * BN + ((uint32_t)((warp & 3) * 32) << 16);
+      const uint32_t acc = tmem + buf * BN + ((uint32_t)row << 16);
 #pragma unroll 1
       for (int g = 0; g < BN / 64; ++g) {
         const int c0 = n * BN + 64 * g;
@@ -331,45 +355,54 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
         const bool mine = turn == set;
         turn = turn + 1 == kMxSets ? 0 : turn + 1;
         if (!mine) continue;
-        if (row == 0) bulk_wait_group_read0();  // the set's last piece has left its buffer
-        set_barrier(set);
-        if (ok) {
+        // a row's 64 outputs per lane, computed while the warp's last piece leaves its buffer; the next 16 columns are on their way
+        uint4 o[8];
+        uint32_t r[2][16];
+        tc_ld_32x32b_x16(acc + 64 * g, r[0]);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t r[32];
-            tc_ld_32x32b_x32(acc + 64 * g + 32 * half, r);
-            tc_wait_ld();
+        for (int i = 0; i < 4; ++i) {
+          ulonglong2 bias[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float v[8];
+          for (int q = 0; q < 4; ++q) bias[q] = make_ulonglong2(0ull, 0ull);
+          if (p.bias != nullptr) {
 #pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r[8 * q + j]);
-              const int c = c0 + 32 * half + 8 * q;
-              if (p.bias != nullptr && c < p.C_out) {
-                const float4 b0 = __ldg(reinterpret_cast<const float4*>(p.bias + c)), b1 = __ldg(reinterpret_cast<const float4*>(p.bias + c) + 1);
-                v[0] += b0.x; v[1] += b0.y; v[2] += b0.z; v[3] += b0.w;
-                v[4] += b1.x; v[5] += b1.y; v[6] += b1.z; v[7] += b1.w;
-              }
-              const uint4 o = make_uint4(activate_pack<ACT>(v[0], v[1]), activate_pack<ACT>(v[2], v[3]), activate_pack<ACT>(v[4], v[5]),
-                                         activate_pack<ACT>(v[6], v[7]));
-              *reinterpret_cast<uint4*>(out + row * 128 + (((4 * half + q) ^ (row & 7)) << 4)) = o;
-            }
+            for (int q = 0; q < 4; ++q)  // (columns past the last channel are not stored)
+              bias[q] = __ldg(reinterpret_cast<const ulonglong2*>(p.bias + min(c0 + 16 * i + 4 * q, p.C_out - 4)));
           }
-          fence_proxy_async_smem();
+          tc_wait_ld_x16(r[i & 1]);
+          if (i < 3) tc_ld_32x32b_x16(acc + 64 * g + 16 * (i + 1), r[(i + 1) & 1]);
+          uint32_t w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float lo, hi;
+            unsigned long long v;
+            asm("add.rn.f32x2 %0, %1, %2;"
+                : "=l"(v)
+                : "l"(f32x2(__uint_as_float(r[i & 1][2 * j]), __uint_as_float(r[i & 1][2 * j + 1]))), "l"(j & 1 ? bias[j >> 1].y : bias[j >> 1].x));
+            split2(v, lo, hi);
+            w[j] = activate_pack<ACT>(lo, hi);
+          }
+          o[2 * i] = make_uint4(w[0], w[1], w[2], w[3]);
+          o[2 * i + 1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
-        set_barrier(set);
-        if (row == 0 && ok) {
-          tma_store_2d(&tm_y, out, c0, m * 128);
+        if (lane == 0) bulk_wait_group_read0();
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(out + lane * 128 + ((q ^ (lane & 7)) << 4)) = o[q];
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_2d(&tm_y, out, c0, m * 128 + row);
           bulk_commit_group();
         }
       }
       tc_fence_before();
       __syncwarp();
-      if ((threadIdx.x & 31) == 0) mbar_arrive(acc_empty + buf);
+      if (lane == 0) mbar_arrive(acc_empty + buf);
       buf ^= 1u;
       if (buf == 0) acc_phase ^= 1u;
     }
-    if (row == 0) bulk_wait_group_read0();
+    if (lane == 0) bulk_wait_group_read0();
   }
 
   tc_fence_before();
@@ -381,7 +414,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mxfp4_kernel(const __grid_const
     if (threadIdx.x == 0 && p.dev_status != nullptr) atomicExch(p.dev_status, (int)SSCONV_ERR_TIMEOUT);
     __syncthreads();
   }
-  if (warp == kMxIssuer) {
+  if (warp == T::kIssuer) {
     tc_fence_after();
     tmem_dealloc(tmem, T::kTmem);
   }
@@ -405,15 +438,22 @@ EncodeFn encoder() {
   }
   return f;
 }
-// A matrix of `rows` rows of `inner` elements, copied in boxes of 128 bytes x box_rows in the 128-byte swizzle.
-bool encode_matrix(EncodeFn f, CUtensorMap* map, CUtensorMapDataType type, int element, const void* base, int64_t inner, int64_t rows, int box_rows) {
+// A matrix of `rows` rows of `inner` elements, copied in boxes of `width` (32, 64 or 128) bytes x box_rows in the swizzle of that
+// width.  (Lines of 128 bytes in L2: promoted to 256 bytes, rows of 48 bytes were fetched several times over, 401408 x 96 -> 384
+// 112 us instead of 90; and boxes that reach past the rows' ends are slow: 128-byte ones on those rows 67.6 us for 192 channels,
+// on rows of 128 bytes 40.7.)
+bool encode_matrix(EncodeFn f, CUtensorMap* map, CUtensorMapDataType type, int element, const void* base, int64_t inner, int64_t rows, int width,
+                   int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)inner * element};
-  const cuuint32_t box[2] = {(cuuint32_t)(128 / element), (cuuint32_t)box_rows}, ones[2] = {1, 1};
-  return f(map, type, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint32_t box[2] = {(cuuint32_t)(width / element), (cuuint32_t)box_rows}, ones[2] = {1, 1};
+  const CUtensorMapSwizzle swizzle = width == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                                     : width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                                   : CU_TENSOR_MAP_SWIZZLE_32B;
+  return f(map, type, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-using MxKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, MxParams);
+using MxKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, MxParams);
 template <int BN>
 MxKernel mx_kernel(int act, int* smem) {
   *smem = MxTile<BN>::kSmem;
@@ -459,22 +499,40 @@ int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const 
   int smem = 0;
   const int act = activation_of(d.flags);
   const MxKernel kernel = bn == 192 ? mx_kernel<192>(act, &smem) : bn == 128 ? mx_kernel<128>(act, &smem) : mx_kernel<64>(act, &smem);
-  const EncodeFn encode = encoder();
-  if (encode == nullptr) return SSCONV_ERR_CUDA;
-  CUtensorMap tm_x, tm_w, tm_y;
   const int64_t row_bytes = (int64_t)gx.blocks * 16;
-  if (!encode_matrix(encode, &tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x_codes, row_bytes, rows, 128) ||
-      !encode_matrix(encode, &tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, w_codes, row_bytes, d.C_out, bn) ||
-      !encode_matrix(encode, &tm_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, y, d.C_out, rows, 128))
-    return SSCONV_ERR_CUDA;
-  MxParams p = {static_cast<const uint8_t*>(x_scales), static_cast<const uint8_t*>(w_scales),
-                (d.flags & SSCONV_FLAG_BIAS) ? bias : nullptr, dev_status, (int)gx.row_tiles, (d.C_out + bn - 1) / bn, (int)gw.row_tiles,
-                d.C_out, gx.chunks, (gx.blocks + 1) / 2};
+  MxParams p = {};
+  p.x_scales = static_cast<const uint8_t*>(x_scales);
+  p.w_scales = static_cast<const uint8_t*>(w_scales);
+  p.bias = (d.flags & SSCONV_FLAG_BIAS) ? bias : nullptr;
+  p.dev_status = dev_status;
+  p.m_tiles = (int)gx.row_tiles;
+  p.n_tiles = (d.C_out + bn - 1) / bn;
+  p.w_tiles = (int)gw.row_tiles;
+  p.C_out = d.C_out;
+  p.chunks = gx.chunks;
+  p.steps = (gx.blocks + 1) / 2;
+  const int tail = (int)((row_bytes - 1) % 128 + 1), stages = (p.steps + 3) / 4;
+  p.tail_bytes = tail <= 32 ? 32 : tail <= 64 ? 64 : 128;
+  p.tail_desc = tail <= 32 ? kDescHiSw32 : tail <= 64 ? kDescHiSw64 : kDescHiSw128;
   const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
   if (tiles > 0x7FFFFFFF - 4096) return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  const EncodeFn encode = encoder();
+  if (encode == nullptr) return SSCONV_ERR_CUDA;
+  CUtensorMap tm_x, tm_w, tm_x_tail, tm_w_tail, tm_y;
+  const auto codes = [&](CUtensorMap* map, const void* base, int64_t n, int width, int box_rows) {
+    return encode_matrix(encode, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, row_bytes, n, width, box_rows);
+  };
+  if (!codes(&tm_x_tail, x_codes, rows, p.tail_bytes, 128) || !codes(&tm_w_tail, w_codes, d.C_out, p.tail_bytes, bn) ||
+      !encode_matrix(encode, &tm_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, y, d.C_out, rows, 128, 32))
+    return SSCONV_ERR_CUDA;
+  tm_x = tm_x_tail;
+  tm_w = tm_w_tail;
+  if (stages > 1 && p.tail_bytes != 128 && (!codes(&tm_x, x_codes, rows, 128, 128) || !codes(&tm_w, w_codes, d.C_out, 128, bn)))
+    return SSCONV_ERR_CUDA;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SSCONV_ERR_CUDA;
   count_launch();
-  return launch_dependent_smem(kernel, (unsigned)(tiles < sms ? tiles : sms), kMxThreads, smem, st, tm_x, tm_w, tm_y, p) == cudaSuccess
+  return launch_dependent_smem(kernel, (unsigned)(tiles < sms ? tiles : sms), MxTile<64>::kThreads, smem, st, tm_x, tm_w, tm_x_tail, tm_w_tail, tm_y, p) ==
+                 cudaSuccess
              ? SSCONV_OK
              : SSCONV_ERR_CUDA;
 }

@@ -620,7 +620,7 @@ Cut cut_backward(const ssconv_resnorm_t& d) {
 
 cudaError_t launch_resnorm(const ssconv_resnorm_t& d, const ResnormTensors& t, cudaStream_t st) {
   const int C8 = d.C / 8;
-  const Team team = team_for(C8, 4);
+  const Team team = team_for(C8, 2);
   ForwardParams p = {t, (int)d.rows, d.rows_per_gate < d.rows ? (int)d.rows_per_gate : (int)d.rows, C8, team.lanes,
                      d.post == SSCONV_NORM_LAYER, d.pre == SSCONV_NORM_LAYER, d.scale, d.eps};
   const bool post = d.post != SSCONV_NORM_NONE, pre = d.pre != SSCONV_NORM_NONE && t.y != nullptr;
