@@ -5,7 +5,8 @@
 // DRAM-bound, or short.
 //
 // A row is held in the registers of a team of threads, V pieces of 8 channels each: part of a warp for few channels, a whole
-// block for many.  Sums along a row go through shuffles, and through shared memory where the team has several warps.
+// block for many.  Sums along a row go through shuffles, and through shared memory where the team has several warps.  A thread's
+// next rows are on their way into shared memory meanwhile, into slots that only this thread reads: no barriers, no registers.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -64,6 +65,27 @@ __device__ __forceinline__ void params8(const float* p, int piece, bool live, fl
   const ulonglong2 a = reinterpret_cast<const ulonglong2*>(p)[2 * piece], b = reinterpret_cast<const ulonglong2*>(p)[2 * piece + 1];
   v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
 }
+// A vector of parameters as a thread uses it: with one piece per thread the piece stays in registers, else it is loaded (from L1)
+// for every row.
+template <bool HELD>
+struct Params {
+  const float* p;
+  float otherwise;
+  Pair held[4];
+  __device__ __forceinline__ void set(const float* from, float without, int piece, bool live) {
+    p = from;
+    otherwise = without;
+    if (HELD) params8(from, piece, live, without, held);
+  }
+  __device__ __forceinline__ void get(int piece, bool live, Pair (&v)[4]) const {
+    if (HELD) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = held[j];
+    } else {
+      params8(p, piece, live, otherwise, v);
+    }
+  }
+};
 __device__ __forceinline__ void store_pairs(float* p, int piece, const Pair (&v)[4]) {
   reinterpret_cast<ulonglong2*>(p)[2 * piece] = make_ulonglong2(v[0], v[1]);
   reinterpret_cast<ulonglong2*>(p)[2 * piece + 1] = make_ulonglong2(v[2], v[3]);
@@ -105,9 +127,16 @@ struct TeamSum {
     }
   }
   __device__ __forceinline__ void operator()(float& a) {
-    float unused = 0.0f;
     if (BLOCK) {
-      (*this)(a, unused);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+      float* s = scratch + 32 * half;
+      half ^= 1;
+      const int warps = blockDim.x >> 5;
+      if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = a;
+      __syncthreads();
+      a = 0.0f;
+      for (int i = 0; i < warps; ++i) a += s[i];
     } else {
       for (int o = lanes >> 1; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
     }
@@ -145,79 +174,134 @@ __device__ __forceinline__ void row_statistics(const Pair (&v)[V][4], const bool
   rstd = rsqrtf(t * inv_c + eps);
 }
 
+constexpr int kCrewThreads = 256;  // of a block whose teams are parts of warps
+
+// A thread's slots of 16 bytes for rows that are on their way: DEPTH rows of SLOTS pieces.  The threads' slots of one piece follow
+// each other: with all slots of a thread side by side the copies took 83 us where they now take 59 (401408 x 96 forward).
+template <int SLOTS, int DEPTH, bool BLOCK>
+struct RowRing {
+  uint32_t at, first, last;  // this thread's slot 0 of the row that is read and then filled next; of the first and the last row
+  __device__ __forceinline__ static uint32_t slot_bytes() { return 16u * (BLOCK ? blockDim.x : (uint32_t)kCrewThreads); }
+  __device__ __forceinline__ RowRing(const void* smem) {
+    at = first = smem_u32(smem) + 16 * threadIdx.x;
+    last = first + (DEPTH - 1) * SLOTS * slot_bytes();
+  }
+  // (nothing is read for a piece that is not there: the slot gets zeros)
+  __device__ __forceinline__ void fetch(int slot, const uint4* src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + slot * slot_bytes()), "l"(src), "r"(bytes) : "memory");
+  }
+  __device__ __forceinline__ void next_row() {
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    at = at == last ? first : at + SLOTS * slot_bytes();
+  }
+  // Once the row that is DEPTH - 1 behind the last one fetched has arrived; that is the one next to be filled again.
+  __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory"); }
+  __device__ __forceinline__ uint4 read(int slot) const {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "r"(at + slot * slot_bytes())
+                 : "memory");
+    return v;
+  }
+};
+constexpr int kForwardDepth = 3;
+__host__ __device__ constexpr int backward_depth(int V) { return V == 1 ? 3 : 2; }
+constexpr int forward_smem(int V, int threads) { return kForwardDepth * 2 * V * 16 * threads; }
+constexpr int kMostSlots = 160 * 1024;  // bytes of any block's slots
+constexpr int backward_smem(int V, int threads) { return backward_depth(V) * (4 * V + 1) * 16 * threads; }
+
 struct ForwardParams {
   ResnormTensors t;
   int rows, rows_per_gate, C8, lanes;
+  int crew_rows;              // consecutive rows of a crew (a warp with its teams, or a block)
   int post_layer, pre_layer;
   float scale, eps;
 };
 
 template <int V, bool BLOCK, bool POST, bool PRE>
-__global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_kernel(const ForwardParams p) {
+__global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(const ForwardParams p) {
+  extern __shared__ __align__(16) uint8_t slots[];
   __shared__ float scratch[64];
   grid_launch_dependents();
   const int lanes = BLOCK ? blockDim.x : p.lanes;
   const int sub = BLOCK ? threadIdx.x : threadIdx.x & (lanes - 1);
-  const int per_block = BLOCK ? 1 : blockDim.x / lanes;
-  const int step = gridDim.x * per_block;
+  const int teams = BLOCK ? 1 : 32 / lanes, team = BLOCK ? 0 : (threadIdx.x & 31) / lanes;
   const float inv_c = 1.0f / (float)(8 * p.C8);
   TeamSum<BLOCK> sum{scratch, lanes};
-  const uint4* x = static_cast<const uint4*>(p.t.x);
-  const uint4* b = static_cast<const uint4*>(p.t.b);
+  RowRing<2 * V, kForwardDepth, BLOCK> ring(slots);
+  const int mine = sub < p.C8 ? sub : 0;
+  const uint4* x = static_cast<const uint4*>(p.t.x) + mine;
+  const uint4* b = static_cast<const uint4*>(p.t.b) + mine;
   uint4* h = static_cast<uint4*>(p.t.h);
   uint4* y = static_cast<uint4*>(p.t.y);
   bool own[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) own[k] = sub + k * lanes < p.C8;
-  grid_dependency_wait();
   // (a warp's teams go on together: its first row decides)
-  int row = BLOCK ? blockIdx.x : blockIdx.x * per_block + threadIdx.x / lanes;
-  const int ahead = BLOCK ? 0 : (threadIdx.x & 31) / lanes;
-  uint4 xn[V], bn[V];
+  const int crew = BLOCK ? blockIdx.x : blockIdx.x * (kCrewThreads / 32) + (threadIdx.x >> 5);
+  const int64_t first = (int64_t)crew * p.crew_rows;
+  const int last = (int)min((int64_t)p.rows, first + p.crew_rows);
+  int row = (int)min((int64_t)p.rows, first) + team;
+  // (in 16-byte pieces of a tensor; x and b are this thread's first piece of row 0)
+  const int64_t stride = (int64_t)teams * p.C8, end = (int64_t)last * p.C8;
+  int64_t coming = (int64_t)row * p.C8;
+  const auto fetch = [&] {
+    const bool there = coming < end;
+    const int64_t at = there ? coming : 0;
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    xn[k] = bn[k] = make_uint4(0u, 0u, 0u, 0u);
-    if (row < p.rows && own[k]) {
-      xn[k] = x[(int64_t)row * p.C8 + sub + k * lanes];
-      bn[k] = b[(int64_t)row * p.C8 + sub + k * lanes];
+    for (int k = 0; k < V; ++k) {
+      const uint32_t bytes = there && own[k] ? 16u : 0u;
+      ring.fetch(2 * k, x + at + (own[k] ? k * lanes : 0), bytes);
+      ring.fetch(2 * k + 1, b + at + (own[k] ? k * lanes : 0), bytes);
     }
-  }
-  for (; row - ahead < p.rows; row += step) {
-    const bool there = row < p.rows;
+    coming += stride;
+    ring.next_row();
+  };
+  grid_dependency_wait();
+#pragma unroll
+  for (int d = 0; d < kForwardDepth - 1; ++d) fetch();
+  int64_t out = (int64_t)row * p.C8 + sub;
+  constexpr bool kHeld = V == 1;
+  Params<kHeld> gates, post_gamma, post_beta, pre_gamma, pre_beta;
+  gates.set(p.rows_per_gate == 0 ? p.t.gate : nullptr, 1.0f, sub, own[0]);
+  if (POST) post_gamma.set(p.t.post_gamma, 1.0f, sub, own[0]);
+  if (POST) post_beta.set(p.t.post_beta, 0.0f, sub, own[0]);
+  if (PRE) pre_gamma.set(p.t.pre_gamma, 1.0f, sub, own[0]);
+  if (PRE) pre_beta.set(p.t.pre_beta, 0.0f, sub, own[0]);
+  int gates_end = 0;  // the first row with other gates
+  for (; row - team < last; row += teams, out += stride) {
+    const bool there = row < last;
+    fetch();
+    ring.wait();
     Pair bv[V][4], hv[V][4];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      unpack8(bn[k], bv[k]);
-      unpack8(xn[k], hv[k]);
-    }
-    const int64_t next = (int64_t)row + step;
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      xn[k] = bn[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (next < p.rows && own[k]) {
-        xn[k] = x[next * p.C8 + sub + k * lanes];
-        bn[k] = b[next * p.C8 + sub + k * lanes];
-      }
+      unpack8(ring.read(2 * k), hv[k]);
+      unpack8(ring.read(2 * k + 1), bv[k]);
     }
     float4 stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (POST) row_statistics(bv, own, p.post_layer, inv_c, p.eps, sum, stats.x, stats.y);
-    const float* gate = p.t.gate;
-    if (gate != nullptr && p.rows_per_gate > 0 && there) gate += (int64_t)(row / p.rows_per_gate) * (8 * p.C8);
+    if (p.rows_per_gate > 0 && there && row >= gates_end) {
+      const int image = row / p.rows_per_gate;
+      gates_end = (int)min((int64_t)p.rows, (int64_t)(image + 1) * p.rows_per_gate);
+      gates.set(p.t.gate != nullptr ? p.t.gate + (int64_t)image * (8 * p.C8) : p.t.gate, 1.0f, sub, own[0]);
+    }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const int piece = sub + k * lanes;
       Pair g[4];
-      params8(gate, piece, own[k], 1.0f, g);
+      gates.get(piece, own[k], g);
       if (POST) {
         Pair a[4], c[4];
-        params8(p.t.post_gamma, piece, own[k], 1.0f, a);
-        params8(p.t.post_beta, piece, own[k], 0.0f, c);
+        post_gamma.get(piece, own[k], a);
+        post_beta.get(piece, own[k], c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) bv[k][j] = fma2(mul2(add2(bv[k][j], both(-stats.x)), both(stats.y)), a[j], c[j]);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) hv[k][j] = own[k] ? fma2(g[j], bv[k][j], mul2(both(p.scale), hv[k][j])) : 0ull;
-      if (there && own[k] && h != nullptr) h[(int64_t)row * p.C8 + piece] = pack8(hv[k]);
+      if (there && own[k] && h != nullptr) h[out + k * lanes] = pack8(hv[k]);
     }
     if (PRE) {
       row_statistics(hv, own, p.pre_layer, inv_c, p.eps, sum, stats.z, stats.w);
@@ -225,11 +309,11 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_kernel(const Forwar
       for (int k = 0; k < V; ++k) {
         const int piece = sub + k * lanes;
         Pair a[4], c[4];
-        params8(p.t.pre_gamma, piece, own[k], 1.0f, a);
-        params8(p.t.pre_beta, piece, own[k], 0.0f, c);
+        pre_gamma.get(piece, own[k], a);
+        pre_beta.get(piece, own[k], c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) hv[k][j] = fma2(mul2(add2(hv[k][j], both(-stats.z)), both(stats.w)), a[j], c[j]);
-        if (there && own[k]) y[(int64_t)row * p.C8 + piece] = pack8(hv[k]);
+        if (there && own[k]) y[out + k * lanes] = pack8(hv[k]);
       }
     }
     if (p.t.stats != nullptr && there && sub == 0) reinterpret_cast<float4*>(p.t.stats)[row] = stats;
@@ -263,16 +347,10 @@ struct BackwardParams {
   float* unit_sums;           // [units][C]
 };
 
-// A row as it was loaded.
-template <int V>
-struct RawRow {
-  uint4 x[V], b[V], dh[V], dy[V];
-  float4 stats;
-};
-
 template <int V, bool BLOCK, bool POST, bool PRE>
-__global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(const BackwardParams p) {
-  extern __shared__ float rows_of_warps[];  // [warps][C], of warp crews
+__global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_kernel(const BackwardParams p) {
+  extern __shared__ __align__(16) uint8_t slots[];
+  float* rows_of_warps = reinterpret_cast<float*>(slots);  // [warps][C], of warp crews, in the end
   __shared__ float scratch[64];
   grid_launch_dependents();
   const int lanes = BLOCK ? blockDim.x : p.lanes;
@@ -283,10 +361,13 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
   const int C = 8 * p.C8;
   const float inv_c = 1.0f / (float)C;
   TeamSum<BLOCK> sum{scratch, lanes};
-  const uint4* x = static_cast<const uint4*>(p.t.x);
-  const uint4* b = static_cast<const uint4*>(p.t.b);
-  const uint4* dh = static_cast<const uint4*>(p.g.dh);
-  const uint4* dy = static_cast<const uint4*>(p.g.dy);
+  constexpr int kDepth = backward_depth(V), kStats = 4 * V;  // slots: b, x, dy, dh of each piece, and the row's statistics
+  RowRing<4 * V + 1, kDepth, BLOCK> ring(slots);
+  const int mine0 = sub < p.C8 ? sub : 0;
+  const uint4* x = static_cast<const uint4*>(p.t.x) + mine0;
+  const uint4* b = static_cast<const uint4*>(p.t.b) + mine0;
+  const uint4* dh = static_cast<const uint4*>(p.g.dh) + mine0;
+  const uint4* dy = static_cast<const uint4*>(p.g.dy) + mine0;
   uint4* dx = static_cast<uint4*>(p.g.dx);
   uint4* db = static_cast<uint4*>(p.g.db);
   bool own[V];
@@ -309,77 +390,91 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
     const int first = image * p.gate_rows + (unit - image * p.units_per_gate) * p.unit_rows;
     return Place{unit, image, first, (int)min((long long)p.rows, min((long long)(image + 1) * p.gate_rows, (long long)first + p.unit_rows))};
   };
-  const auto load = [&](const Place& at, RawRow<V>& raw) {
+  const auto go_on = [&](Place& at) {
+    at.row += teams;
+    if (at.row >= at.end) at = start_of(at.unit + crews);
+  };
+  const auto fetch = [&](Place& at) {
     const int row = at.row + team;
-    const bool there = at.unit < p.units && row < at.end;
-    if ((POST || PRE) && there) raw.stats = reinterpret_cast<const float4*>(p.t.stats)[row];
+    const bool there = row < at.end && at.unit < p.units;
+    if (POST || PRE) ring.fetch(kStats, reinterpret_cast<const uint4*>(p.t.stats) + (there ? row : 0), there ? 16u : 0u);
+    const int64_t i0 = there ? (int64_t)row * p.C8 : 0;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      raw.x[k] = raw.b[k] = raw.dh[k] = raw.dy[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (there && own[k]) {
-        const int64_t i = (int64_t)row * p.C8 + sub + k * lanes;
-        raw.b[k] = b[i];
-        if (PRE) {
-          raw.x[k] = x[i];
-          raw.dy[k] = dy[i];
-        }
-        if (dh != nullptr) raw.dh[k] = dh[i];
+      const uint32_t bytes = there && own[k] ? 16u : 0u;
+      const int64_t i = i0 + (own[k] ? k * lanes : 0);
+      ring.fetch(4 * k, b + i, bytes);
+      if (PRE) {
+        ring.fetch(4 * k + 1, x + i, bytes);
+        ring.fetch(4 * k + 2, dy + i, bytes);
       }
+      if (p.g.dh != nullptr) ring.fetch(4 * k + 3, dh + i, bytes);
     }
+    ring.next_row();
+    if (at.unit < p.units) go_on(at);
   };
 
   grid_dependency_wait();
-  Place at = start_of(blockIdx.x * crews_per_block + (BLOCK ? 0 : threadIdx.x >> 5));
-  RawRow<V> coming;
-  coming.stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  load(at, coming);
+  Place at = start_of(blockIdx.x * crews_per_block + (BLOCK ? 0 : threadIdx.x >> 5)), coming = at;
+#pragma unroll
+  for (int d = 0; d < kDepth - 1; ++d) fetch(coming);
+  constexpr bool kHeld = V == 1;
+  Params<kHeld> gates, post_gamma, post_beta, pre_gamma;
+  const auto set_gates = [&] { gates.set(p.t.gate != nullptr && p.image_gates ? p.t.gate + (int64_t)at.image * C : p.t.gate, 1.0f, sub, own[0]); };
+  if (at.unit < p.units) set_gates();
+  if (POST) post_gamma.set(p.t.post_gamma, 1.0f, sub, own[0]);
+  if (POST) post_beta.set(p.t.post_beta, 0.0f, sub, own[0]);
+  if (PRE) pre_gamma.set(p.t.pre_gamma, 1.0f, sub, own[0]);
   while (at.unit < p.units) {
-    const RawRow<V> raw = coming;
+    fetch(coming);
     Place next = at;
-    next.row += teams;
-    if (next.row >= at.end) next = start_of(at.unit + crews);
-    load(next, coming);
+    go_on(next);
+    ring.wait();
+    float4 stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (POST || PRE) {
+      const uint4 v = ring.read(kStats);
+      stats = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+    }
     const int row = at.row + team;
     const bool there = row < at.end;
-    const float* gate = p.t.gate;
-    if (gate != nullptr && p.image_gates) gate += (int64_t)at.image * C;
+    const int64_t out = (int64_t)row * p.C8 + sub;
 
     Pair d[V][4], hat[V][4], pv[V][4];  // pv: bhat with a first norm, else b itself
     Pair s1 = 0, s2 = 0;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const int piece = sub + k * lanes;
-      unpack8(raw.b[k], pv[k]);
-      unpack8(raw.dh[k], d[k]);
+      unpack8(ring.read(4 * k), pv[k]);
+      unpack8(p.g.dh != nullptr ? ring.read(4 * k + 3) : make_uint4(0u, 0u, 0u, 0u), d[k]);
       if (POST) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) pv[k][j] = mul2(add2(pv[k][j], both(-raw.stats.x)), both(raw.stats.y));
+        for (int j = 0; j < 4; ++j) pv[k][j] = mul2(add2(pv[k][j], both(-stats.x)), both(stats.y));
       }
       if (PRE) {
         Pair gv[4], a[4], c[4], g[4];
-        unpack8(raw.x[k], hat[k]);
-        unpack8(raw.dy[k], gv);
-        params8(gate, piece, own[k], 1.0f, g);
+        unpack8(ring.read(4 * k + 1), hat[k]);
+        unpack8(ring.read(4 * k + 2), gv);
+        gates.get(piece, own[k], g);
         if (POST) {
-          params8(p.t.post_gamma, piece, own[k], 1.0f, a);
-          params8(p.t.post_beta, piece, own[k], 0.0f, c);
+          post_gamma.get(piece, own[k], a);
+          post_beta.get(piece, own[k], c);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const Pair pj = POST ? fma2(pv[k][j], a[j], c[j]) : pv[k][j];
           const Pair h = fma2(g[j], pj, mul2(both(p.scale), hat[k][j]));
-          hat[k][j] = mul2(add2(h, both(-raw.stats.z)), both(raw.stats.w));
+          hat[k][j] = mul2(add2(h, both(-stats.z)), both(stats.w));
           acc[kPreGamma][k][j] = fma2(gv[j], hat[k][j], acc[kPreGamma][k][j]);
           acc[kPreBeta][k][j] = add2(acc[kPreBeta][k][j], gv[j]);
         }
-        params8(p.t.pre_gamma, piece, own[k], 1.0f, a);
+        pre_gamma.get(piece, own[k], a);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const Pair q = mul2(gv[j], a[j]);
           s1 = add2(s1, q);
           s2 = fma2(q, hat[k][j], s2);
           // dh plus what the norm hands back, but for the means
-          d[k][j] = fma2(q, both(raw.stats.w), d[k][j]);
+          d[k][j] = fma2(q, both(stats.w), d[k][j]);
         }
       }
     }
@@ -387,8 +482,8 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
     if (PRE) {
       float m = sum_of(s1), q = sum_of(s2);
       sum(m, q);
-      from_mean = both(p.pre_layer ? -raw.stats.w * (m * inv_c) : 0.0f);
-      from_hat = both(-raw.stats.w * (q * inv_c));
+      from_mean = both(p.pre_layer ? -stats.w * (m * inv_c) : 0.0f);
+      from_hat = both(-stats.w * (q * inv_c));
     }
     Pair t1 = 0, t2 = 0;
 #pragma unroll
@@ -403,12 +498,12 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
         Pair o[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = mul2(both(p.scale), d[k][j]);
-        dx[(int64_t)row * p.C8 + piece] = pack8(o);
+        dx[out + k * lanes] = pack8(o);
       }
-      params8(gate, piece, own[k], 1.0f, g);
+      gates.get(piece, own[k], g);
       if (POST) {
-        params8(p.t.post_gamma, piece, own[k], 1.0f, a);
-        params8(p.t.post_beta, piece, own[k], 0.0f, c);
+        post_gamma.get(piece, own[k], a);
+        post_beta.get(piece, own[k], c);
       }
       if (there && own[k]) {
 #pragma unroll
@@ -429,35 +524,39 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 256) resnorm_backward_kernel(con
     if (POST) {
       float m = sum_of(t1), q = sum_of(t2);
       sum(m, q);
-      from_mean = both(p.post_layer ? -raw.stats.y * (m * inv_c) : 0.0f);
-      from_hat = both(-raw.stats.y * (q * inv_c));
+      from_mean = both(p.post_layer ? -stats.y * (m * inv_c) : 0.0f);
+      from_hat = both(-stats.y * (q * inv_c));
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       if (POST) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) d[k][j] = fma2(d[k][j], both(raw.stats.y), fma2(pv[k][j], from_hat, from_mean));
+        for (int j = 0; j < 4; ++j) d[k][j] = fma2(d[k][j], both(stats.y), fma2(pv[k][j], from_hat, from_mean));
       }
-      if (there && own[k] && db != nullptr) db[(int64_t)row * p.C8 + sub + k * lanes] = pack8(d[k]);
+      if (there && own[k] && db != nullptr) db[out + k * lanes] = pack8(d[k]);
     }
 
     if (next.unit != at.unit && p.image_gates && p.g.dgate != nullptr) {
-      float* out = p.units_per_gate == 1 ? p.g.dgate + (int64_t)at.image * C : p.unit_sums + (int64_t)at.unit * C;
+      float* to = p.units_per_gate == 1 ? p.g.dgate + (int64_t)at.image * C : p.unit_sums + (int64_t)at.unit * C;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         if (!BLOCK)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             for (int o = 16; o >= lanes; o >>= 1) acc[kGate][k][j] = add2(acc[kGate][k][j], __shfl_xor_sync(0xFFFFFFFFu, acc[kGate][k][j], o));
-        if (own[k] && team == 0) store_pairs(out, sub + k * lanes, acc[kGate][k]);
+        if (own[k] && team == 0) store_pairs(to, sub + k * lanes, acc[kGate][k]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[kGate][k][j] = 0;
       }
     }
+    const bool other = next.image != at.image;
     at = next;
+    if (other && at.unit < p.units) set_gates();
   }
 
-  // What is left in the registers, summed over the block's warps and teams.
+  // What is left in the registers, summed over the block's warps and teams (in the slots' memory: every copy into it is over).
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (!BLOCK) __syncthreads();
   float* mine = p.block_sums + (int64_t)blockIdx.x * kSums * C;
 #pragma unroll
   for (int a = 0; a < kSums; ++a) {
@@ -549,27 +648,56 @@ int power_of_two_from(int n) {
   while (p < n) p <<= 1;
   return p;
 }
-// Up to `warp_pieces` pieces per lane a row is part of a warp, else a block's.
-Team team_for(int C8, int warp_pieces) {
-  if (C8 <= 32) return {false, 1, power_of_two_from(C8), 256};
-  if (C8 <= 32 * warp_pieces) return {false, (C8 + 31) / 32, 32, 256};
+// One piece per thread: parameters and sums of its channels then stay in its registers, and what is done once per row is
+// spread over the most threads.  us, forward / with gradients: 401408 x 96 one piece on 12 of 16 lanes 61 / 146, three pieces on
+// 4 lanes 64 / 160; 12017 x 1000 with both norms one piece on 128 threads 25 / 67, two on 64 30 / 97, four on a warp 33 / 107.
+// Rows of more than 4096 channels take two pieces.
+Team team_for(int C8) {
+  if (C8 <= 32) return {false, 1, power_of_two_from(C8), kCrewThreads};
   const int V = C8 <= 512 ? 1 : 2;
   const int threads = (((C8 + V - 1) / V) + 31) / 32 * 32;
   return {true, V, threads, threads};
 }
 
+// Allows a kernel its dynamic shared memory, once per device, and says how many of its blocks an SM then holds.
+struct Resident {
+  std::atomic<uint64_t> key{0};  // the kernel's address and the threads of its blocks
+  std::atomic<int> blocks[64];
+};
+int resident_blocks(const void* kernel, int threads, int smem) {
+  static Resident known[512];
+  int dev = 0, blocks = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  const uint64_t key = (uint64_t)reinterpret_cast<uintptr_t>(kernel) ^ ((uint64_t)threads << 50);
+  Resident* r = nullptr;
+  for (Resident& k : known) {
+    uint64_t at = k.key.load(std::memory_order_relaxed);
+    if (at == 0 && k.key.compare_exchange_strong(at, key)) at = key;
+    if (at == key) {
+      r = &k;
+      break;
+    }
+  }
+  if (r != nullptr) blocks = r->blocks[dev].load(std::memory_order_relaxed);
+  if (blocks == 0) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSlots) != cudaSuccess) return 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, threads, smem) != cudaSuccess || blocks <= 0) return 0;
+    if (r != nullptr) r->blocks[dev].store(blocks, std::memory_order_relaxed);
+  }
+  return blocks;
+}
+
+static_assert(forward_smem(2, 512) <= kMostSlots && backward_smem(1, 512) <= kMostSlots && backward_smem(2, 512) <= kMostSlots, "");
+
 template <bool POST, bool PRE>
 void (*forward_kernel(const Team& t))(ForwardParams) {
-  if (t.block) return t.V == 1 ? resnorm_kernel<1, true, POST, PRE> : resnorm_kernel<2, true, POST, PRE>;
-  return t.V == 1   ? resnorm_kernel<1, false, POST, PRE>
-         : t.V == 2 ? resnorm_kernel<2, false, POST, PRE>
-         : t.V == 3 ? resnorm_kernel<3, false, POST, PRE>
-                    : resnorm_kernel<4, false, POST, PRE>;
+  return !t.block ? resnorm_kernel<1, false, POST, PRE> : t.V == 1 ? resnorm_kernel<1, true, POST, PRE> : resnorm_kernel<2, true, POST, PRE>;
 }
 template <bool POST, bool PRE>
 void (*backward_kernel(const Team& t))(BackwardParams) {
-  if (t.block) return t.V == 1 ? resnorm_backward_kernel<1, true, POST, PRE> : resnorm_backward_kernel<2, true, POST, PRE>;
-  return t.V == 1 ? resnorm_backward_kernel<1, false, POST, PRE> : resnorm_backward_kernel<2, false, POST, PRE>;
+  return !t.block   ? resnorm_backward_kernel<1, false, POST, PRE>
+         : t.V == 1 ? resnorm_backward_kernel<1, true, POST, PRE>
+                    : resnorm_backward_kernel<2, true, POST, PRE>;
 }
 
 // How the backward pass is cut: units, and blocks (the scratch is sized by them).
@@ -578,12 +706,12 @@ struct Cut {
   int units, unit_rows, units_per_gate, gate_rows, blocks, images;
   bool image_gates;
 };
-constexpr int kBackwardWarps = 16;       // per SM, of crews at work at once (half as many with two pieces per lane of a warp)
+constexpr int kBackwardWarps = 16;       // per SM, of crews at work at once
 constexpr int kRowsPerTeam = 4;          // of a unit, at least: its sums are written once
 
 Cut cut_backward(const ssconv_resnorm_t& d) {
   Cut c;
-  c.team = team_for(d.C / 8, 2);
+  c.team = team_for(d.C / 8);
   c.image_gates = d.rows_per_gate > 0;
   const int64_t rows = d.rows;
   c.gate_rows = (int)(c.image_gates && d.rows_per_gate < rows ? d.rows_per_gate : rows);
@@ -591,8 +719,7 @@ Cut cut_backward(const ssconv_resnorm_t& d) {
   const int crew_warps = c.team.block ? c.team.threads / 32 : 1;
   const int teams = c.team.block ? 1 : 32 / c.team.lanes;
   const int crews_per_block = c.team.block ? 1 : c.team.threads / 32;
-  const int warps = !c.team.block && c.team.V == 2 ? kBackwardWarps / 2 : kBackwardWarps;
-  const int64_t most = (int64_t)device_sms() * (warps / crew_warps > 0 ? warps / crew_warps : 1);
+  const int64_t most = (int64_t)device_sms() * (kBackwardWarps / crew_warps > 0 ? kBackwardWarps / crew_warps : 1);
   // Units per row of gates: as many as keep the crew with the most rows short, fewer where it makes no difference.
   const int64_t worth = (c.gate_rows + teams * kRowsPerTeam - 1) / (teams * kRowsPerTeam);
   const int64_t all = most / c.images < 1 ? 1 : most / c.images;
@@ -620,17 +747,29 @@ Cut cut_backward(const ssconv_resnorm_t& d) {
 
 cudaError_t launch_resnorm(const ssconv_resnorm_t& d, const ResnormTensors& t, cudaStream_t st) {
   const int C8 = d.C / 8;
-  const Team team = team_for(C8, 2);
-  ForwardParams p = {t, (int)d.rows, d.rows_per_gate < d.rows ? (int)d.rows_per_gate : (int)d.rows, C8, team.lanes,
-                     d.post == SSCONV_NORM_LAYER, d.pre == SSCONV_NORM_LAYER, d.scale, d.eps};
+  const Team team = team_for(C8);
   const bool post = d.post != SSCONV_NORM_NONE, pre = d.pre != SSCONV_NORM_NONE && t.y != nullptr;
   const auto kernel = post ? (pre ? forward_kernel<true, true>(team) : forward_kernel<true, false>(team))
                            : (pre ? forward_kernel<false, true>(team) : forward_kernel<false, false>(team));
-  const int per_block = team.block ? 1 : team.threads / team.lanes;
-  const int64_t blocks = (d.rows + per_block - 1) / per_block;
-  const int64_t most = (int64_t)device_sms() * (team.block ? 1024 / team.threads : 4);
+  const int smem = forward_smem(team.V, team.threads);
+  const int teams = team.block ? 1 : 32 / team.lanes, crews_per_block = team.block ? 1 : team.threads / 32;
+  const int64_t most = (int64_t)device_sms() * resident_blocks((const void*)kernel, team.threads, smem) * crews_per_block;
+  if (most == 0) return cudaErrorUnknown;
+  const int64_t turns = (d.rows + most * teams - 1) / (most * teams);
+  ForwardParams p = {};
+  p.t = t;
+  p.rows = (int)d.rows;
+  p.rows_per_gate = (int)(d.rows_per_gate < d.rows ? d.rows_per_gate : d.rows);
+  p.C8 = C8;
+  p.lanes = team.lanes;
+  p.crew_rows = (int)(turns * teams);
+  p.post_layer = d.post == SSCONV_NORM_LAYER;
+  p.pre_layer = d.pre == SSCONV_NORM_LAYER;
+  p.scale = d.scale;
+  p.eps = d.eps;
+  const int64_t crews = (d.rows + p.crew_rows - 1) / p.crew_rows;
   count_launch();
-  return launch_dependent(kernel, (unsigned)(blocks < most ? blocks : most), team.threads, st, p);
+  return launch_dependent_smem(kernel, (unsigned)((crews + crews_per_block - 1) / crews_per_block), team.threads, smem, st, p);
 }
 
 size_t resnorm_scratch(const ssconv_resnorm_t& d) {
@@ -663,7 +802,8 @@ cudaError_t launch_resnorm_backward(const ssconv_resnorm_t& d, const ResnormTens
   const bool post = d.post != SSCONV_NORM_NONE, pre = d.pre != SSCONV_NORM_NONE;
   const auto kernel = post ? (pre ? backward_kernel<true, true>(c.team) : backward_kernel<true, false>(c.team))
                            : (pre ? backward_kernel<false, true>(c.team) : backward_kernel<false, false>(c.team));
-  const size_t smem = c.team.block ? 0 : (size_t)(c.team.threads / 32) * d.C * sizeof(float);
+  const int smem = backward_smem(c.team.V, c.team.threads);  // (more than a row of sums per warp)
+  if (resident_blocks((const void*)kernel, c.team.threads, smem) == 0) return cudaErrorUnknown;
   count_launch();
   cudaError_t e = launch_dependent_smem(kernel, (unsigned)c.blocks, c.team.threads, smem, st, p);
   if (e != cudaSuccess) return e;
