@@ -55,11 +55,12 @@ __device__ __forceinline__ uint32_t pack2(Pair v) {
   return pack_bf16x2<false>(lo, hi);
 }
 __device__ __forceinline__ uint4 pack8(const Pair (&v)[4]) { return make_uint4(pack2(v[0]), pack2(v[1]), pack2(v[2]), pack2(v[3])); }
-// 8 of a vector of parameters, `otherwise` where there is none.
+// 8 of a vector of parameters, `otherwise` where there is no vector; zeros for a piece past the row, whose values then stay zero.
 __device__ __forceinline__ void params8(const float* p, int piece, bool live, float otherwise, Pair (&v)[4]) {
   if (p == nullptr || !live) {
+    const float o = live ? otherwise : 0.0f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = both(otherwise);
+    for (int j = 0; j < 4; ++j) v[j] = both(o);
     return;
   }
   const ulonglong2 a = reinterpret_cast<const ulonglong2*>(p)[2 * piece], b = reinterpret_cast<const ulonglong2*>(p)[2 * piece + 1];
@@ -69,8 +70,8 @@ __device__ __forceinline__ void params8(const float* p, int piece, bool live, fl
 // for every row.
 template <bool HELD>
 struct Params {
-  const float* p;
-  float otherwise;
+  const float* p = nullptr;
+  float otherwise = 0.0f;
   Pair held[4];
   __device__ __forceinline__ void set(const float* from, float without, int piece, bool live) {
     p = from;
@@ -91,84 +92,94 @@ __device__ __forceinline__ void store_pairs(float* p, int piece, const Pair (&v)
   reinterpret_cast<ulonglong2*>(p)[2 * piece + 1] = make_ulonglong2(v[2], v[3]);
 }
 
-// Sums over a team's threads, known to all of them afterwards.  Teams of several warps are whole blocks; their sums alternate
-// between two halves of the scratch, so that one barrier per sum is enough: a thread writes into a half again only after the
-// barrier of the sum in between, which every reader of that half passes after it has read.
-template <bool BLOCK>
+// A team: LANES threads of a warp (a power of two), or all of a block's (LANES = 32 then).
+//
+// Sums over a block go through 16 slots per value, one per warp, zeros where there is no warp.  Two sets of them are used in turn,
+// so that one barrier per sum is enough: a thread writes into a set again only after the barrier of the sum in between, which
+// every reader of that set passes after it has read.
+template <int LANES, bool BLOCK>
 struct TeamSum {
   float* scratch;  // [2][2][16]
-  int lanes;       // of a team within a warp
-  int half = 0;
-  __device__ __forceinline__ void operator()(float& a, float& b) {
+  int warps;
+  __device__ __forceinline__ void begin(float* smem) {
+    scratch = smem;
+    warps = blockDim.x >> 5;
     if (BLOCK) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-        b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
-      }
-      float* s = scratch + 32 * half;
-      half ^= 1;
-      const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-      if ((threadIdx.x & 31) == 0) {
-        s[warp] = a;
-        s[16 + warp] = b;
-      }
+      if (threadIdx.x < 32) scratch[threadIdx.x] = scratch[32 + threadIdx.x] = 0.0f;
       __syncthreads();
-      a = b = 0.0f;
-      for (int i = 0; i < warps; ++i) {
-        a += s[i];
-        b += s[16 + i];
-      }
-    } else {
-      for (int o = lanes >> 1; o > 0; o >>= 1) {
-        a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-        b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
-      }
     }
   }
-  __device__ __forceinline__ void operator()(float& a) {
-    if (BLOCK) {
+  __device__ __forceinline__ static void lanes(float& a) {
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-      float* s = scratch + 32 * half;
-      half ^= 1;
-      const int warps = blockDim.x >> 5;
+    for (int o = LANES >> 1; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+  }
+  __device__ __forceinline__ static float four(const float4& v) { return (v.x + v.y) + (v.z + v.w); }
+  __device__ __forceinline__ float all_warps(const float* s) const {
+    const float4* v = reinterpret_cast<const float4*>(s);
+    float t = four(v[0]);
+    if (warps > 4) t += four(v[1]);
+    if (warps > 8) t += four(v[2]) + four(v[3]);
+    return t;
+  }
+  __device__ __forceinline__ float* take_set() {
+    float* s = scratch;
+    // (the two sets are 128 bytes apart, at a multiple of 256)
+    scratch = reinterpret_cast<float*>(reinterpret_cast<uintptr_t>(scratch) ^ 128u);
+    return s;
+  }
+  __device__ __forceinline__ void operator()(float& a) {
+    lanes(a);
+    if (BLOCK) {
+      float* s = take_set();
       if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = a;
       __syncthreads();
-      a = 0.0f;
-      for (int i = 0; i < warps; ++i) a += s[i];
-    } else {
-      for (int o = lanes >> 1; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+      a = all_warps(s);
+    }
+  }
+  __device__ __forceinline__ void operator()(float& a, float& b) {
+    lanes(a);
+    lanes(b);
+    if (BLOCK) {
+      float* s = take_set();
+      if ((threadIdx.x & 31) == 0) {
+        s[threadIdx.x >> 5] = a;
+        s[16 + (threadIdx.x >> 5)] = b;
+      }
+      __syncthreads();
+      a = all_warps(s);
+      b = all_warps(s + 16);
     }
   }
 };
 
-// Mean (0 for RMS) and 1 / deviation of a row; two passes over the registers, so that a mean far from zero costs no digits.
-template <int V, bool BLOCK>
+// Mean (0 for RMS) and 1 / deviation of a row; two passes over the registers, so that a mean far from zero costs no digits.  (A
+// block's warps could put sums about their own means together with one barrier instead of two: 3000 x 4096 78 us instead of 40.)
+template <int LANES, int V, bool BLOCK>
 __device__ __forceinline__ void row_statistics(const Pair (&v)[V][4], const bool (&live)[V], bool layer, float inv_c, float eps,
-                                               TeamSum<BLOCK>& sum, float& mean, float& rstd) {
+                                               TeamSum<LANES, BLOCK>& sum, float& mean, float& rstd) {
   mean = 0.0f;
   if (layer) {
-    Pair s = 0;
+    Pair s = v[0][0];
 #pragma unroll
     for (int k = 0; k < V; ++k)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s = add2(s, v[k][j]);  // (zeros in pieces past the row)
-    float t = sum_of(s);
-    sum(t);
-    mean = t * inv_c;
+      for (int j = k == 0 ? 1 : 0; j < 4; ++j) s = add2(s, v[k][j]);  // (zeros in pieces past the row)
+    mean = sum_of(s);
+    sum(mean);
+    mean *= inv_c;
   }
   Pair q = 0;
   const Pair less = both(-mean);
 #pragma unroll
-  for (int k = 0; k < V; ++k)
-    if (live[k]) {
+  for (int k = 0; k < V; ++k) {
+    Pair r = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const Pair d = add2(v[k][j], less);
-        q = fma2(d, d, q);
-      }
+    for (int j = 0; j < 4; ++j) {
+      const Pair d = add2(v[k][j], less);
+      r = fma2(d, d, r);
     }
+    q = add2(q, live[k] ? r : 0ull);
+  }
   float t = sum_of(q);
   sum(t);
   rstd = rsqrtf(t * inv_c + eps);
@@ -186,8 +197,8 @@ struct RowRing {
     at = first = smem_u32(smem) + 16 * threadIdx.x;
     last = first + (DEPTH - 1) * SLOTS * slot_bytes();
   }
-  // (nothing is read for a piece that is not there: the slot gets zeros)
-  __device__ __forceinline__ void fetch(int slot, const uint4* src, uint32_t bytes) {
+  // (nothing is read where bytes = 0: the slot gets zeros)
+  __device__ __forceinline__ void fetch(int slot, const void* src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + slot * slot_bytes()), "l"(src), "r"(bytes) : "memory");
   }
   __device__ __forceinline__ void next_row() {
@@ -208,60 +219,59 @@ struct RowRing {
 constexpr int kForwardDepth = 3;
 __host__ __device__ constexpr int backward_depth(int V) { return V == 1 ? 3 : 2; }
 constexpr int forward_smem(int V, int threads) { return kForwardDepth * 2 * V * 16 * threads; }
-constexpr int kMostSlots = 160 * 1024;  // bytes of any block's slots
 constexpr int backward_smem(int V, int threads) { return backward_depth(V) * (4 * V + 1) * 16 * threads; }
+constexpr int kMostSlots = 160 * 1024;  // bytes of any block's slots
 
 struct ForwardParams {
   ResnormTensors t;
-  int rows, rows_per_gate, C8, lanes;
+  int rows, rows_per_gate, C8;
   int crew_rows;              // consecutive rows of a crew (a warp with its teams, or a block)
   int post_layer, pre_layer;
   float scale, eps;
 };
 
-template <int V, bool BLOCK, bool POST, bool PRE>
+template <int LANES, int V, bool BLOCK, bool POST, bool PRE>
 __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(const ForwardParams p) {
   extern __shared__ __align__(16) uint8_t slots[];
-  __shared__ float scratch[64];
+  __shared__ __align__(256) float scratch[64];
   grid_launch_dependents();
-  const int lanes = BLOCK ? blockDim.x : p.lanes;
-  const int sub = BLOCK ? threadIdx.x : threadIdx.x & (lanes - 1);
-  const int teams = BLOCK ? 1 : 32 / lanes, team = BLOCK ? 0 : (threadIdx.x & 31) / lanes;
-  const float inv_c = 1.0f / (float)(8 * p.C8);
-  TeamSum<BLOCK> sum{scratch, lanes};
+  const int run = BLOCK ? blockDim.x : LANES;  // pieces between a thread's pieces
+  const int sub = BLOCK ? threadIdx.x : threadIdx.x & (LANES - 1);
+  constexpr int kTeams = BLOCK ? 1 : 32 / LANES;
+  const int team = BLOCK ? 0 : (threadIdx.x & 31) / LANES;
+  const int C8 = p.C8;
+  const float inv_c = 1.0f / (float)(8 * C8);
+  TeamSum<LANES, BLOCK> sum;
+  sum.begin(scratch);
   RowRing<2 * V, kForwardDepth, BLOCK> ring(slots);
-  const int mine = sub < p.C8 ? sub : 0;
-  const uint4* x = static_cast<const uint4*>(p.t.x) + mine;
-  const uint4* b = static_cast<const uint4*>(p.t.b) + mine;
-  uint4* h = static_cast<uint4*>(p.t.h);
-  uint4* y = static_cast<uint4*>(p.t.y);
   bool own[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) own[k] = sub + k * lanes < p.C8;
+  for (int k = 0; k < V; ++k) own[k] = sub + k * run < C8;
+
   // (a warp's teams go on together: its first row decides)
   const int crew = BLOCK ? blockIdx.x : blockIdx.x * (kCrewThreads / 32) + (threadIdx.x >> 5);
   const int64_t first = (int64_t)crew * p.crew_rows;
   const int last = (int)min((int64_t)p.rows, first + p.crew_rows);
   int row = (int)min((int64_t)p.rows, first) + team;
-  // (in 16-byte pieces of a tensor; x and b are this thread's first piece of row 0)
-  const int64_t stride = (int64_t)teams * p.C8, end = (int64_t)last * p.C8;
-  int64_t coming = (int64_t)row * p.C8;
+  // bytes from the tensors' starts: of this thread's piece in the row that is fetched next, and in the one that is worked on
+  const int64_t stride = (int64_t)kTeams * C8 * 16;
+  int64_t coming = ((int64_t)row * C8 + sub) * 16, here = coming;
+  int coming_row = row;
   const auto fetch = [&] {
-    const bool there = coming < end;
-    const int64_t at = there ? coming : 0;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const uint32_t bytes = there && own[k] ? 16u : 0u;
-      ring.fetch(2 * k, x + at + (own[k] ? k * lanes : 0), bytes);
-      ring.fetch(2 * k + 1, b + at + (own[k] ? k * lanes : 0), bytes);
+      const bool mine = coming_row < last && own[k];
+      const int64_t at = mine ? coming + k * 16 * run : 0;
+      ring.fetch(2 * k, static_cast<const uint8_t*>(p.t.x) + at, mine ? 16u : 0u);
+      ring.fetch(2 * k + 1, static_cast<const uint8_t*>(p.t.b) + at, mine ? 16u : 0u);
     }
     coming += stride;
+    coming_row += kTeams;
     ring.next_row();
   };
   grid_dependency_wait();
 #pragma unroll
   for (int d = 0; d < kForwardDepth - 1; ++d) fetch();
-  int64_t out = (int64_t)row * p.C8 + sub;
   constexpr bool kHeld = V == 1;
   Params<kHeld> gates, post_gamma, post_beta, pre_gamma, pre_beta;
   gates.set(p.rows_per_gate == 0 ? p.t.gate : nullptr, 1.0f, sub, own[0]);
@@ -269,8 +279,9 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
   if (POST) post_beta.set(p.t.post_beta, 0.0f, sub, own[0]);
   if (PRE) pre_gamma.set(p.t.pre_gamma, 1.0f, sub, own[0]);
   if (PRE) pre_beta.set(p.t.pre_beta, 0.0f, sub, own[0]);
-  int gates_end = 0;  // the first row with other gates
-  for (; row - team < last; row += teams, out += stride) {
+  int gates_end = p.rows_per_gate > 0 ? 0 : p.rows;  // the first row with other gates
+  const Pair scale = both(p.scale);
+  for (; row - team < last; row += kTeams, here += stride) {
     const bool there = row < last;
     fetch();
     ring.wait();
@@ -281,15 +292,15 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
       unpack8(ring.read(2 * k + 1), bv[k]);
     }
     float4 stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (POST) row_statistics(bv, own, p.post_layer, inv_c, p.eps, sum, stats.x, stats.y);
-    if (p.rows_per_gate > 0 && there && row >= gates_end) {
+    if (POST) row_statistics<LANES, V, BLOCK>(bv, own, p.post_layer, inv_c, p.eps, sum, stats.x, stats.y);
+    if (there && row >= gates_end) {
       const int image = row / p.rows_per_gate;
       gates_end = (int)min((int64_t)p.rows, (int64_t)(image + 1) * p.rows_per_gate);
-      gates.set(p.t.gate != nullptr ? p.t.gate + (int64_t)image * (8 * p.C8) : p.t.gate, 1.0f, sub, own[0]);
+      gates.set(p.t.gate != nullptr ? p.t.gate + (int64_t)image * (8 * C8) : p.t.gate, 1.0f, sub, own[0]);
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int piece = sub + k * lanes;
+      const int piece = sub + k * run;
       Pair g[4];
       gates.get(piece, own[k], g);
       if (POST) {
@@ -300,23 +311,23 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
         for (int j = 0; j < 4; ++j) bv[k][j] = fma2(mul2(add2(bv[k][j], both(-stats.x)), both(stats.y)), a[j], c[j]);
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) hv[k][j] = own[k] ? fma2(g[j], bv[k][j], mul2(both(p.scale), hv[k][j])) : 0ull;
-      if (there && own[k] && h != nullptr) h[out + k * lanes] = pack8(hv[k]);
+      for (int j = 0; j < 4; ++j) hv[k][j] = fma2(g[j], bv[k][j], mul2(scale, hv[k][j]));
+      if (there && own[k] && p.t.h != nullptr) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.t.h) + here + k * 16 * run) = pack8(hv[k]);
     }
     if (PRE) {
-      row_statistics(hv, own, p.pre_layer, inv_c, p.eps, sum, stats.z, stats.w);
+      row_statistics<LANES, V, BLOCK>(hv, own, p.pre_layer, inv_c, p.eps, sum, stats.z, stats.w);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const int piece = sub + k * lanes;
+        const int piece = sub + k * run;
         Pair a[4], c[4];
         pre_gamma.get(piece, own[k], a);
         pre_beta.get(piece, own[k], c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) hv[k][j] = fma2(mul2(add2(hv[k][j], both(-stats.z)), both(stats.w)), a[j], c[j]);
-        if (there && own[k]) y[out + k * lanes] = pack8(hv[k]);
+        if (there && own[k]) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.t.y) + here + k * 16 * run) = pack8(hv[k]);
       }
     }
-    if (p.t.stats != nullptr && there && sub == 0) reinterpret_cast<float4*>(p.t.stats)[row] = stats;
+    if (sub == 0 && there && p.t.stats != nullptr) reinterpret_cast<float4*>(p.t.stats)[row] = stats;
   }
 }
 
@@ -340,39 +351,45 @@ struct BackwardParams {
   ResnormGradients g;
   int rows, gate_rows;        // gate_rows: rows with the same gates (all of them for shared or no gates)
   int units, unit_rows, units_per_gate;
-  int C8, lanes;
+  int C8;
   int post_layer, pre_layer, image_gates;
   float scale;
   float* block_sums;          // [blocks][kSums][C]
   float* unit_sums;           // [units][C]
 };
 
-template <int V, bool BLOCK, bool POST, bool PRE>
+// A place among a crew's rows: a unit, the first of the teams' rows in it, and the unit's end.
+struct Place {
+  int unit, image, row, end;
+};
+__device__ __forceinline__ Place start_of(const BackwardParams& p, int unit) {
+  const int image = unit / p.units_per_gate;
+  const int64_t first = (int64_t)image * p.gate_rows + (int64_t)(unit - image * p.units_per_gate) * p.unit_rows;
+  const int64_t end = min((int64_t)p.rows, min((int64_t)(image + 1) * p.gate_rows, first + p.unit_rows));
+  return {unit, image, (int)min((int64_t)p.rows, first), (int)end};
+}
+
+template <int LANES, int V, bool BLOCK, bool POST, bool PRE>
 __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_kernel(const BackwardParams p) {
   extern __shared__ __align__(16) uint8_t slots[];
   float* rows_of_warps = reinterpret_cast<float*>(slots);  // [warps][C], of warp crews, in the end
-  __shared__ float scratch[64];
+  __shared__ __align__(256) float scratch[64];
   grid_launch_dependents();
-  const int lanes = BLOCK ? blockDim.x : p.lanes;
-  const int sub = BLOCK ? threadIdx.x : threadIdx.x & (lanes - 1);
-  const int teams = BLOCK ? 1 : 32 / lanes, team = BLOCK ? 0 : (threadIdx.x & 31) / lanes;
-  const int crews_per_block = BLOCK ? 1 : blockDim.x >> 5;
-  const int crews = gridDim.x * crews_per_block;
-  const int C = 8 * p.C8;
+  const int run = BLOCK ? blockDim.x : LANES;
+  const int sub = BLOCK ? threadIdx.x : threadIdx.x & (LANES - 1);
+  constexpr int kTeams = BLOCK ? 1 : 32 / LANES;
+  const int team = BLOCK ? 0 : (threadIdx.x & 31) / LANES;
+  constexpr int kCrewsPerBlock = BLOCK ? 1 : kCrewThreads / 32;
+  const int crews = gridDim.x * kCrewsPerBlock;
+  const int C8 = p.C8, C = 8 * C8;
   const float inv_c = 1.0f / (float)C;
-  TeamSum<BLOCK> sum{scratch, lanes};
+  TeamSum<LANES, BLOCK> sum;
+  sum.begin(scratch);
   constexpr int kDepth = backward_depth(V), kStats = 4 * V;  // slots: b, x, dy, dh of each piece, and the row's statistics
   RowRing<4 * V + 1, kDepth, BLOCK> ring(slots);
-  const int mine0 = sub < p.C8 ? sub : 0;
-  const uint4* x = static_cast<const uint4*>(p.t.x) + mine0;
-  const uint4* b = static_cast<const uint4*>(p.t.b) + mine0;
-  const uint4* dh = static_cast<const uint4*>(p.g.dh) + mine0;
-  const uint4* dy = static_cast<const uint4*>(p.g.dy) + mine0;
-  uint4* dx = static_cast<uint4*>(p.g.dx);
-  uint4* db = static_cast<uint4*>(p.g.db);
   bool own[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) own[k] = sub + k * lanes < p.C8;
+  for (int k = 0; k < V; ++k) own[k] = sub + k * run < C8;
   Pair acc[kSums][V][4];
 #pragma unroll
   for (int a = 0; a < kSums; ++a)
@@ -380,42 +397,34 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
     for (int k = 0; k < V; ++k)
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[a][k][j] = 0;
+  const bool with_dh = p.g.dh != nullptr;
 
-  // A place among a crew's rows: a unit, the first of the teams' rows in it, and the unit's end.
-  struct Place {
-    int unit, image, row, end;
-  };
-  const auto start_of = [&](int unit) {
-    const int image = unit / p.units_per_gate;
-    const int first = image * p.gate_rows + (unit - image * p.units_per_gate) * p.unit_rows;
-    return Place{unit, image, first, (int)min((long long)p.rows, min((long long)(image + 1) * p.gate_rows, (long long)first + p.unit_rows))};
-  };
   const auto go_on = [&](Place& at) {
-    at.row += teams;
-    if (at.row >= at.end) at = start_of(at.unit + crews);
+    at.row += kTeams;
+    if (at.row >= at.end) at = start_of(p, at.unit + crews);
   };
   const auto fetch = [&](Place& at) {
     const int row = at.row + team;
     const bool there = row < at.end && at.unit < p.units;
-    if (POST || PRE) ring.fetch(kStats, reinterpret_cast<const uint4*>(p.t.stats) + (there ? row : 0), there ? 16u : 0u);
-    const int64_t i0 = there ? (int64_t)row * p.C8 : 0;
+    if (POST || PRE) ring.fetch(kStats, p.t.stats + 4 * (int64_t)(there ? row : 0), there ? 16u : 0u);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const uint32_t bytes = there && own[k] ? 16u : 0u;
-      const int64_t i = i0 + (own[k] ? k * lanes : 0);
-      ring.fetch(4 * k, b + i, bytes);
+      const bool mine = there && own[k];
+      const int64_t i = mine ? ((int64_t)row * C8 + sub + k * run) * 16 : 0;
+      const uint32_t bytes = mine ? 16u : 0u;
+      ring.fetch(4 * k, static_cast<const uint8_t*>(p.t.b) + i, bytes);
       if (PRE) {
-        ring.fetch(4 * k + 1, x + i, bytes);
-        ring.fetch(4 * k + 2, dy + i, bytes);
+        ring.fetch(4 * k + 1, static_cast<const uint8_t*>(p.t.x) + i, bytes);
+        ring.fetch(4 * k + 2, static_cast<const uint8_t*>(p.g.dy) + i, bytes);
       }
-      if (p.g.dh != nullptr) ring.fetch(4 * k + 3, dh + i, bytes);
+      if (with_dh) ring.fetch(4 * k + 3, static_cast<const uint8_t*>(p.g.dh) + i, bytes);
     }
     ring.next_row();
     if (at.unit < p.units) go_on(at);
   };
 
   grid_dependency_wait();
-  Place at = start_of(blockIdx.x * crews_per_block + (BLOCK ? 0 : threadIdx.x >> 5)), coming = at;
+  Place at = start_of(p, blockIdx.x * kCrewsPerBlock + (BLOCK ? 0 : threadIdx.x >> 5)), coming = at;
 #pragma unroll
   for (int d = 0; d < kDepth - 1; ++d) fetch(coming);
   constexpr bool kHeld = V == 1;
@@ -425,6 +434,7 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
   if (POST) post_gamma.set(p.t.post_gamma, 1.0f, sub, own[0]);
   if (POST) post_beta.set(p.t.post_beta, 0.0f, sub, own[0]);
   if (PRE) pre_gamma.set(p.t.pre_gamma, 1.0f, sub, own[0]);
+  const Pair scale = both(p.scale);
   while (at.unit < p.units) {
     fetch(coming);
     Place next = at;
@@ -435,17 +445,17 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
       const uint4 v = ring.read(kStats);
       stats = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
     }
-    const int row = at.row + team;
-    const bool there = row < at.end;
-    const int64_t out = (int64_t)row * p.C8 + sub;
+    const bool there = at.row + team < at.end;
+    const int64_t here = ((int64_t)(at.row + team) * C8 + sub) * 16;
 
+    // (pieces past the row and rows past the unit are zeros with parameters or gradients of zero: nothing of them is left in a sum)
     Pair d[V][4], hat[V][4], pv[V][4];  // pv: bhat with a first norm, else b itself
     Pair s1 = 0, s2 = 0;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int piece = sub + k * lanes;
+      const int piece = sub + k * run;
       unpack8(ring.read(4 * k), pv[k]);
-      unpack8(p.g.dh != nullptr ? ring.read(4 * k + 3) : make_uint4(0u, 0u, 0u, 0u), d[k]);
+      unpack8(with_dh ? ring.read(4 * k + 3) : make_uint4(0u, 0u, 0u, 0u), d[k]);
       if (POST) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) pv[k][j] = mul2(add2(pv[k][j], both(-stats.x)), both(stats.y));
@@ -462,7 +472,7 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const Pair pj = POST ? fma2(pv[k][j], a[j], c[j]) : pv[k][j];
-          const Pair h = fma2(g[j], pj, mul2(both(p.scale), hat[k][j]));
+          const Pair h = fma2(g[j], pj, mul2(scale, hat[k][j]));
           hat[k][j] = mul2(add2(h, both(-stats.z)), both(stats.w));
           acc[kPreGamma][k][j] = fma2(gv[j], hat[k][j], acc[kPreGamma][k][j]);
           acc[kPreBeta][k][j] = add2(acc[kPreBeta][k][j], gv[j]);
@@ -488,36 +498,38 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
     Pair t1 = 0, t2 = 0;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int piece = sub + k * lanes;
+      const int piece = sub + k * run;
+      const bool mine = there && own[k];
       Pair a[4], c[4], g[4];
       if (PRE) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) d[k][j] = add2(fma2(hat[k][j], from_hat, from_mean), d[k][j]);
+        for (int j = 0; j < 4; ++j) {
+          d[k][j] = add2(fma2(hat[k][j], from_hat, from_mean), d[k][j]);
+        }
       }
-      if (there && own[k] && dx != nullptr) {
+      if (mine && p.g.dx != nullptr) {
         Pair o[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = mul2(both(p.scale), d[k][j]);
-        dx[out + k * lanes] = pack8(o);
+        for (int j = 0; j < 4; ++j) o[j] = mul2(scale, d[k][j]);
+        *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.g.dx) + here + k * 16 * run) = pack8(o);
       }
       gates.get(piece, own[k], g);
       if (POST) {
         post_gamma.get(piece, own[k], a);
         post_beta.get(piece, own[k], c);
       }
-      if (there && own[k]) {
+      if (mine)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const Pair pj = POST ? fma2(pv[k][j], a[j], c[j]) : pv[k][j];
-          acc[kGate][k][j] = fma2(d[k][j], pj, acc[kGate][k][j]);
-          d[k][j] = mul2(d[k][j], g[j]);  // dp from here on
-          if (POST) {
-            acc[kPostGamma][k][j] = fma2(d[k][j], pv[k][j], acc[kPostGamma][k][j]);
-            acc[kPostBeta][k][j] = add2(acc[kPostBeta][k][j], d[k][j]);
-            d[k][j] = mul2(d[k][j], a[j]);
-            t1 = add2(t1, d[k][j]);
-            t2 = fma2(d[k][j], pv[k][j], t2);
-          }
+      for (int j = 0; j < 4; ++j) {
+        const Pair pj = POST ? fma2(pv[k][j], a[j], c[j]) : pv[k][j];
+        acc[kGate][k][j] = fma2(d[k][j], pj, acc[kGate][k][j]);
+        d[k][j] = mul2(d[k][j], g[j]);  // dp from here on
+        if (POST) {
+          acc[kPostGamma][k][j] = fma2(d[k][j], pv[k][j], acc[kPostGamma][k][j]);
+          acc[kPostBeta][k][j] = add2(acc[kPostBeta][k][j], d[k][j]);
+          d[k][j] = mul2(d[k][j], a[j]);
+          t1 = add2(t1, d[k][j]);
+          t2 = fma2(d[k][j], pv[k][j], t2);
         }
       }
     }
@@ -533,18 +545,18 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
 #pragma unroll
         for (int j = 0; j < 4; ++j) d[k][j] = fma2(d[k][j], both(stats.y), fma2(pv[k][j], from_hat, from_mean));
       }
-      if (there && own[k] && db != nullptr) db[out + k * lanes] = pack8(d[k]);
+      if (there && own[k] && p.g.db != nullptr) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.g.db) + here + k * 16 * run) = pack8(d[k]);
     }
 
     if (next.unit != at.unit && p.image_gates && p.g.dgate != nullptr) {
       float* to = p.units_per_gate == 1 ? p.g.dgate + (int64_t)at.image * C : p.unit_sums + (int64_t)at.unit * C;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        if (!BLOCK)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            for (int o = 16; o >= lanes; o >>= 1) acc[kGate][k][j] = add2(acc[kGate][k][j], __shfl_xor_sync(0xFFFFFFFFu, acc[kGate][k][j], o));
-        if (own[k] && team == 0) store_pairs(to, sub + k * lanes, acc[kGate][k]);
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int o = 16; o >= LANES; o >>= 1) acc[kGate][k][j] = add2(acc[kGate][k][j], __shfl_xor_sync(0xFFFFFFFFu, acc[kGate][k][j], o));
+        if (own[k] && team == 0) store_pairs(to, sub + k * run, acc[kGate][k]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[kGate][k][j] = 0;
       }
@@ -568,11 +580,11 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
     float* out = BLOCK ? mine + a * C : rows_of_warps + (threadIdx.x >> 5) * C;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      if (!BLOCK)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          for (int o = 16; o >= lanes; o >>= 1) acc[a][k][j] = add2(acc[a][k][j], __shfl_xor_sync(0xFFFFFFFFu, acc[a][k][j], o));
-      if (own[k] && team == 0) store_pairs(out, sub + k * lanes, acc[a][k]);
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int o = 16; o >= LANES; o >>= 1) acc[a][k][j] = add2(acc[a][k][j], __shfl_xor_sync(0xFFFFFFFFu, acc[a][k][j], o));
+      if (own[k] && team == 0) store_pairs(out, sub + k * run, acc[a][k]);
     }
     if (!BLOCK) {
       __syncthreads();
@@ -689,16 +701,26 @@ int resident_blocks(const void* kernel, int threads, int smem) {
 
 static_assert(forward_smem(2, 512) <= kMostSlots && backward_smem(1, 512) <= kMostSlots && backward_smem(2, 512) <= kMostSlots, "");
 
+// The kernel of a team.
+#define SSCONV_TEAM_KERNEL(kernel)                                                                        \
+  if (t.block) return t.V == 1 ? kernel<32, 1, true, POST, PRE> : kernel<32, 2, true, POST, PRE>;         \
+  switch (t.lanes) {                                                                                      \
+    case 1: return kernel<1, 1, false, POST, PRE>;                                                        \
+    case 2: return kernel<2, 1, false, POST, PRE>;                                                        \
+    case 4: return kernel<4, 1, false, POST, PRE>;                                                        \
+    case 8: return kernel<8, 1, false, POST, PRE>;                                                        \
+    case 16: return kernel<16, 1, false, POST, PRE>;                                                      \
+    default: return kernel<32, 1, false, POST, PRE>;                                                      \
+  }
 template <bool POST, bool PRE>
 void (*forward_kernel(const Team& t))(ForwardParams) {
-  return !t.block ? resnorm_kernel<1, false, POST, PRE> : t.V == 1 ? resnorm_kernel<1, true, POST, PRE> : resnorm_kernel<2, true, POST, PRE>;
+  SSCONV_TEAM_KERNEL(resnorm_kernel)
 }
 template <bool POST, bool PRE>
 void (*backward_kernel(const Team& t))(BackwardParams) {
-  return !t.block   ? resnorm_backward_kernel<1, false, POST, PRE>
-         : t.V == 1 ? resnorm_backward_kernel<1, true, POST, PRE>
-                    : resnorm_backward_kernel<2, true, POST, PRE>;
+  SSCONV_TEAM_KERNEL(resnorm_backward_kernel)
 }
+#undef SSCONV_TEAM_KERNEL
 
 // How the backward pass is cut: units, and blocks (the scratch is sized by them).
 struct Cut {
@@ -761,7 +783,6 @@ cudaError_t launch_resnorm(const ssconv_resnorm_t& d, const ResnormTensors& t, c
   p.rows = (int)d.rows;
   p.rows_per_gate = (int)(d.rows_per_gate < d.rows ? d.rows_per_gate : d.rows);
   p.C8 = C8;
-  p.lanes = team.lanes;
   p.crew_rows = (int)(turns * teams);
   p.post_layer = d.post == SSCONV_NORM_LAYER;
   p.pre_layer = d.pre == SSCONV_NORM_LAYER;
@@ -792,7 +813,6 @@ cudaError_t launch_resnorm_backward(const ssconv_resnorm_t& d, const ResnormTens
   p.unit_rows = c.unit_rows;
   p.units_per_gate = c.units_per_gate;
   p.C8 = d.C / 8;
-  p.lanes = c.team.lanes;
   p.post_layer = d.post == SSCONV_NORM_LAYER;
   p.pre_layer = d.pre == SSCONV_NORM_LAYER;
   p.image_gates = c.image_gates;
