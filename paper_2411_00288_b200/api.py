@@ -849,19 +849,8 @@ def ssconv_dgrad_spread(desc: Desc, dy: torch.Tensor, stream=None) -> torch.Tens
 
 
 # ----------------------------------------------------------------------------- all tensors of a network
-# (These calls and the ones below check and allocate their tensors in the native binding, all for the current stream: another one
-# is made current around them.)
-def _on_stream(call):
-    """`call` with a keyword `stream`: a torch stream to run on, None for the current one."""
-    @functools.wraps(call)
-    def on(*args, stream=None, **kwargs):
-        if stream is None:
-            return call(*args, **kwargs)
-        with torch.cuda.stream(stream):
-            return call(*args, **kwargs)
-    return on
-
-
+# (These calls and the ones below check and allocate their tensors in the native binding, all for the current stream: another one,
+# a torch stream, is made current around them.)
 GRAD_NORM_L2, GRAD_NORM_INF = 0, 1
 
 
@@ -872,30 +861,36 @@ def ssconv_grad_norm_ws_bytes(tensors: int) -> int:
     return int(n.value)
 
 
-@_on_stream
-def ssconv_grad_norm(grads, kind: int = GRAD_NORM_L2, norm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+def ssconv_grad_norm(grads, kind: int = GRAD_NORM_L2, norm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """fp32 [1] on the device: the root of the sum of all squares (GRAD_NORM_L2), or the largest magnitude (GRAD_NORM_INF), of
     a list of fp32 or bf16 tensors (not synchronised)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return ssconv_grad_norm(grads, kind, norm, ws)
     rc, norm = _binding().grad_norm(grads, kind, norm, ws)
     _check("ssconv_grad_norm", rc)
     return norm
 
 
-@_on_stream
-def ssconv_clip_grads(grads, norm: torch.Tensor, max_norm: float, out=None):
+def ssconv_clip_grads(grads, norm: torch.Tensor, max_norm: float, out=None, stream=None):
     """Scale every gradient by min(1, max_norm / (norm + 1e-6)), norm as ssconv_grad_norm wrote it: in place, or into the
     tensors of `out` (of the same types); returns the list of results."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return ssconv_clip_grads(grads, norm, max_norm, out)
     if out is None:
         out = grads
     _check("ssconv_clip_grads", _binding().clip_grads(grads, out, norm, max_norm)[0])
     return out
 
 
-@_on_stream
 def ssconv_adamw_multi(theta, g, m, v, step: int, lr: float = 1.0, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
-                       weight_decay: float = 1e-4, norm: Optional[torch.Tensor] = None, max_norm: float = 1.0) -> None:
+                       weight_decay: float = 1e-4, norm: Optional[torch.Tensor] = None, max_norm: float = 1.0, stream=None) -> None:
     """ssconv_adamw of every tensor of the lists theta, m, v (fp32, modified) with the gradients g (fp32 or bf16); with `norm`
     the gradients are scaled as by ssconv_clip_grads on the way (g itself stays as it is)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return ssconv_adamw_multi(theta, g, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm)
     _check("ssconv_adamw_multi", _binding().adamw_multi(theta, g, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm)[0])
 
 
@@ -915,13 +910,15 @@ def make_resnorm(rows: int, C: int, rows_per_gate: int = 0, post: int = NORM_NON
     return ResNorm(rows, rows_per_gate, C, post, pre, scale, eps)
 
 
-@_on_stream
 def ssconv_residual_norm(desc: ResNorm, x: torch.Tensor, b: torch.Tensor, gate: Optional[torch.Tensor] = None,
                          post_gamma: Optional[torch.Tensor] = None, post_beta: Optional[torch.Tensor] = None,
                          pre_gamma: Optional[torch.Tensor] = None, pre_beta: Optional[torch.Tensor] = None, want_stats: bool = False,
-                         h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None):
+                         h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None, stream=None):
     """(h, y or None, stats or None): h = scale x + gate post(b), y = pre(h), bf16 like x; stats fp32 [rows, 4] for the backward
     call.  gate fp32 [C] or [ceil(rows / rows_per_gate), C]; gammas and betas fp32 [C], None for ones and zeros."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return ssconv_residual_norm(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, want_stats, h, y, stats)
     rc, h, y, stats = _binding().residual_norm(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, want_stats, h, y, stats)
     _check("ssconv_residual_norm", rc)
     return h, y, stats
@@ -946,14 +943,16 @@ def ssconv_residual_norm_ws_bytes(desc: ResNorm) -> int:
     return int(n.value)
 
 
-@_on_stream
 def ssconv_residual_norm_backward(desc: ResNorm, x: torch.Tensor, b: torch.Tensor, stats: Optional[torch.Tensor],
                                   dh: Optional[torch.Tensor], dy: Optional[torch.Tensor], gate: Optional[torch.Tensor] = None,
                                   post_gamma: Optional[torch.Tensor] = None, post_beta: Optional[torch.Tensor] = None,
                                   pre_gamma: Optional[torch.Tensor] = None, pre_beta: Optional[torch.Tensor] = None,
-                                  ws: Optional[torch.Tensor] = None) -> ResNormGrads:
+                                  ws: Optional[torch.Tensor] = None, stream=None) -> ResNormGrads:
     """Gradients from dh and dy (bf16 like x; dh may be None) and the forward call's inputs and stats: dx, db bf16, the others
     fp32 and of their inputs' shapes, one for each gate, gamma and beta that is given."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return ssconv_residual_norm_backward(desc, x, b, stats, dh, dy, gate, post_gamma, post_beta, pre_gamma, pre_beta, ws)
     rc, *grads = _binding().residual_norm_backward(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, stats, dh, dy, ws)
     _check("ssconv_residual_norm_backward", rc)
     return ResNormGrads(*grads)
@@ -967,29 +966,35 @@ def ssconv_sizes_mxfp4(rows: int, C: int) -> Tuple[int, int]:
     return int(a.value), int(b.value)
 
 
-@_on_stream
-def ssconv_quantize_mxfp4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
+def ssconv_quantize_mxfp4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """(codes, scales) uint8 of bf16 x [..., C]: e2m1 elements, one power of two per 32 channels; scales in the tile order that
     ssconv_forward_dense_mxfp4 reads.  Weights [C_out, C_in] are quantised by the same call."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return ssconv_quantize_mxfp4(x, codes, scales)
     rc, codes, scales = _binding().quantize_mxfp4(x, codes, scales)
     _check("ssconv_quantize_mxfp4", rc)
     return codes, scales
 
 
-@_on_stream
-def ssconv_dequantize_mxfp4(codes: torch.Tensor, scales: torch.Tensor, C: int, x: Optional[torch.Tensor] = None) -> torch.Tensor:
+def ssconv_dequantize_mxfp4(codes: torch.Tensor, scales: torch.Tensor, C: int, x: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The bf16 values [..., C] that codes and scales stand for (exact)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return ssconv_dequantize_mxfp4(codes, scales, C, x)
     rc, x = _binding().dequantize_mxfp4(codes, scales, C, x)
     _check("ssconv_dequantize_mxfp4", rc)
     return x
 
 
-@_on_stream
 def ssconv_forward_dense_mxfp4(desc: Desc, x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
                                bias: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
-                               dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+                               dev_status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Point-wise layer on microscaled 4-bit activations and weights (both from ssconv_quantize_mxfp4); bf16 output
     [N,H,W,C_out] (enqueued, not synchronised)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return ssconv_forward_dense_mxfp4(desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status)
     rc, y = _binding().forward_dense_mxfp4(desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status)
     _check("ssconv_forward_dense_mxfp4", rc)
     return y

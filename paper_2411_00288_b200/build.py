@@ -39,7 +39,7 @@ def build_binding(force: bool = False) -> str:
                 os.path.join(t, "include", "torch", "csrc", "api", "include"),
                 os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC"] + ["-I" + i for i in includes] +
-                   [sources[0], "-o", binding, "-L" + os.path.join(t, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
+                   [sources[0], "-o", binding, "-L" + os.path.join(t, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda",
                     "-lc10", "-lc10_cuda", "-L" + _HERE, "-l:libssconv.so", "-Wl,-rpath,$ORIGIN"], check=True)
     return binding
 

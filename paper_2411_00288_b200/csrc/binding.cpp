@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -152,6 +153,7 @@ PyObject* blob(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // (Outputs that are not given are allocated for the current stream.)
 
 bool here(const at::Tensor& t) { return t.is_cuda() && t.is_contiguous() && t.get_device() == c10::cuda::current_device(); }
+bool on(int device, const at::Tensor& t) { return t.is_cuda() && t.is_contiguous() && t.get_device() == device; }
 
 // The address of a tensor of `numel` elements of `type` on the current device, or nullptr for None.
 void* expect(PyObject* o, const char* name, at::ScalarType type, int64_t numel) {
@@ -175,7 +177,7 @@ void* expect(PyObject* o, const char* name, at::ScalarType type, int64_t numel) 
 // A new tensor beside `like` if o is None, o itself otherwise (checked by expect()).
 at::Tensor given_or_new(PyObject* o, at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
   if (o != Py_None) return as_tensor(o);
-  return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+  return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
 }
 void* address(const at::Tensor& t) { return t.numel() != 0 ? t.mutable_data_ptr() : nullptr; }
 
@@ -251,9 +253,11 @@ struct TensorList {
     p.reserve(count);
     n.reserve(count);
     type.reserve(count);
+    int device = -1;
     for (Py_ssize_t i = 0; i < count; ++i) {
       const at::Tensor& t = as_tensor(PySequence_Fast_GET_ITEM(items, i));
-      if (!here(t)) raise(PyExc_ValueError, "tensors must be contiguous and on the current CUDA device");
+      if (i == 0 && t.is_cuda()) device = c10::cuda::current_device();
+      if (!on(device, t)) raise(PyExc_ValueError, "tensors must be contiguous and on the current CUDA device");
       const bool bf16 = t.scalar_type() == at::kBFloat16;
       if (!bf16 && t.scalar_type() != at::kFloat) raise(PyExc_TypeError, "float32 or bfloat16 tensors are expected");
       if (bf16 && !takes_bf16) raise(PyExc_TypeError, "float32 tensors are expected");

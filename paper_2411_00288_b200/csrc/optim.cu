@@ -130,27 +130,28 @@ __device__ __forceinline__ double block_fold(Fold f) {
   return all.value();
 }
 
-template <class Fold, class T>
-__device__ __forceinline__ void fold_chunk(Fold& f, const T* p, int n, int t, int threads) {
+template <int THREADS, class Fold, class T>
+__device__ __forceinline__ void fold_chunk(Fold& f, const T* p, int n, int t) {
   if ((reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
     const int whole = n >> 3;
-    // (two pieces of 8 at a time: four 16-byte loads in flight)
+    // (two pieces of 8 at a time, four 16-byte loads in flight; four where a warp has a chunk to itself)
+    constexpr int kAtOnce = THREADS == 32 ? 4 : 2;
     int i = t;
-    for (; i + threads < whole; i += 2 * threads) {
-      float a[8], b[8];
-      load8(p + 8 * i, a);
-      load8(p + 8 * (i + threads), b);
-      f.add(a);
-      f.add(b);
+    for (; i + (kAtOnce - 1) * THREADS < whole; i += kAtOnce * THREADS) {
+      float v[kAtOnce][8];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) load8(p + 8 * (i + k * THREADS), v[k]);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) f.add(v[k]);
     }
-    if (i < whole) {
-      float a[8];
-      load8(p + 8 * i, a);
-      f.add(a);
+    for (; i < whole; i += THREADS) {
+      float v[8];
+      load8(p + 8 * i, v);
+      f.add(v);
     }
     if (t < (n & 7)) f.add1(load1(p + 8 * whole + t));
   } else {
-    for (int i = t; i < n; i += threads) f.add1(load1(p + i));
+    for (int i = t; i < n; i += THREADS) f.add1(load1(p + i));
   }
 }
 
@@ -165,31 +166,45 @@ __device__ __forceinline__ int chunk_length(const Table& t, int i, int64_t at) {
   return left < (int64_t)t.chunk ? (int)left : (int)t.chunk;
 }
 
-// One partial result per block.  DRAM-bound: 4 (2) bytes per gradient.  ALONE: one block writes the norm itself, its warps
-// taking a chunk each.
-template <class Fold, bool ALONE, int MOST>
-__global__ void __launch_bounds__(ALONE ? 1024 : kOptThreads) grad_norm_kernel(const __grid_constant__ TensorTable<MOST, 1> t, double* partial,
+// One partial result per block.  DRAM-bound: 4 (2) bytes per gradient.  WHOLE: the grid is one cluster of blocks whose warps take
+// a chunk each, and whose first block adds up the others' results in their shared memory and writes the norm: one launch.
+template <class Fold, bool WHOLE, int MOST>
+__global__ void __launch_bounds__(WHOLE ? 1024 : kOptThreads) grad_norm_kernel(const __grid_constant__ TensorTable<MOST, 1> t, double* partial,
                                                                                float* norm) {
+  __shared__ double whole;
   grid_launch_dependents();
   grid_dependency_wait();
-  const int thread = ALONE ? threadIdx.x & 31 : threadIdx.x, threads = ALONE ? 32 : kOptThreads;
+  const int thread = WHOLE ? threadIdx.x & 31 : threadIdx.x;
+  constexpr int kThreads = WHOLE ? 32 : kOptThreads;
   Fold f;
-  for (uint32_t c = ALONE ? threadIdx.x >> 5 : blockIdx.x; c < t.chunks; c += ALONE ? 32 : gridDim.x) {
+  for (uint32_t c = WHOLE ? (threadIdx.x >> 5) * gridDim.x + blockIdx.x : blockIdx.x; c < t.chunks; c += WHOLE ? 32 * gridDim.x : gridDim.x) {
     const int i = tensor_of(t, c);
     const int64_t at = chunk_start(t, i, c);
     const int len = chunk_length(t, i, at);
     if (t.n[i] < 0)
-      fold_chunk(f, static_cast<const __nv_bfloat16*>(t.p[0][i]) + at, len, thread, threads);
+      fold_chunk<kThreads>(f, static_cast<const __nv_bfloat16*>(t.p[0][i]) + at, len, thread);
     else
-      fold_chunk(f, static_cast<const float*>(t.p[0][i]) + at, len, thread, threads);
+      fold_chunk<kThreads>(f, static_cast<const float*>(t.p[0][i]) + at, len, thread);
   }
   const double v = block_fold(f);
-  if (threadIdx.x == 0) {
-    if (ALONE)
-      *norm = Fold::norm(v);
-    else
-      partial[blockIdx.x] = v;
+  if (!WHOLE) {
+    if (threadIdx.x == 0) partial[blockIdx.x] = v;
+    return;
   }
+  if (threadIdx.x == 0) whole = v;
+  cluster_arrive();
+  cluster_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    Fold all;
+    for (uint32_t r = 0; r < gridDim.x; ++r) {
+      double other;
+      asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(other) : "r"(map_to_cta(smem_u32(&whole), r)) : "memory");
+      all.join(other);
+    }
+    *norm = Fold::norm(all.value());
+  }
+  cluster_arrive();  // (no block leaves while its result may still be read)
+  cluster_wait();
 }
 
 // The partial results together, in an order that depends on their number alone.
@@ -331,8 +346,8 @@ __global__ void __launch_bounds__(kOptThreads) adamw_multi_kernel(const __grid_c
 // ---------------------------------------------------------------------------------------
 // Calls of few tensors have a small argument (a launch copies it), others one of up to kMany tensors; more take several launches.
 constexpr int kFew = 32, kMany = 384;
-// Norms of little are taken by one block, in one launch.
-constexpr uint32_t kAloneChunk = 1024, kAloneChunks = 64;
+// Norms of little are taken by one cluster, in one launch: a chunk of up to 2048 elements for each of its warps.
+constexpr uint32_t kWholeChunk = 2048, kWholeBlocks = 8, kWholeChunks = 32 * kWholeBlocks;
 
 // Elements of a chunk: many where there is much to do (a block's work should outweigh finding it), few where the blocks of
 // the chip would otherwise go without.
@@ -375,9 +390,24 @@ static cudaError_t grad_norm_with(const void* const* g, const int64_t* n, const 
                                   cudaStream_t st) {
   TensorTable<MOST, 1> t;
   void* const* const arrays[1] = {const_cast<void* const*>(g)};
-  if (fill_table(t, arrays, n, type, tensors, kAloneChunk, 0) == tensors && t.chunks <= kAloneChunks) {
+  if (fill_table(t, arrays, n, type, tensors, kWholeChunk, 0) == tensors && t.chunks <= kWholeChunks) {
+    // as many blocks as there are chunks for their warps
+    uint32_t blocks = 1;
+    while (blocks < kWholeBlocks && 32 * blocks < t.chunks) blocks <<= 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = blocks;
+    cfg.blockDim = 1024;
+    cfg.stream = st;
+    cudaLaunchAttribute attrs[2];
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = blocks;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = blocks > 1 ? 2 : 1;
     count_launch();
-    return launch_dependent(grad_norm_kernel<Fold, true, MOST>, 1, 1024, st, t, partial, norm);
+    return cudaLaunchKernelEx(&cfg, grad_norm_kernel<Fold, true, MOST>, t, partial, norm);
   }
   const uint32_t most = blocks_per_launch(), chunk = chunk_elements(n, tensors);
   int at = 0, parts = 0;
