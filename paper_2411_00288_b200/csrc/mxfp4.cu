@@ -131,19 +131,20 @@ __global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* c
 // K in stages of 256 channels (128 bytes of codes per row, the 128-byte swizzle; two scale images per 128 rows).  One thread block
 // per SM walks over tiles, channels first, so that the blocks at work at a time share few rows of x; two accumulators, so that a
 // tile's epilogue runs beside the next one's MMAs.  The epilogue's pieces (64 channels) go to kMxSets sets of four warps in turn;
-// each warp stages and stores its 32 rows by itself.  Two more warps are the producer and the MMA issuer.
+// each warp stages and stores its 32 rows by itself.  Three more warps are the producer, the MMA issuer and the one that moves
+// the scales into TMEM.
 // ---------------------------------------------------------------------------------------
 constexpr long long kMxWaitLimit = 4000000000LL;  // cycles: about 2 s
 constexpr int kMxStoreBytes = 32 * 128;           // staged outputs of a warp: 32 pixels x 64 channels of bf16
 constexpr int kMxSets = 3;
 constexpr int kMxMostSmem = 227 * 1024;
 
-template <int BN>
+template <int BN, bool PAIR>
 struct MxTile {
-  static constexpr int kProducer = 4 * kMxSets, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 1);
+  static constexpr int kProducer = 4 * kMxSets, kIssuer = kProducer + 1, kScaler = kProducer + 2, kThreads = 32 * (kScaler + 1);
   static constexpr int kStagedBytes = 4 * kMxSets * kMxStoreBytes;
   static constexpr int kScaleTiles = BN > 128 ? 2 : 1;  // images along the tile's channels
-  static constexpr int kBytesA = 128 * 128, kBytesB = BN * 128, kBytesScales = 1024 * (1 + kScaleTiles);
+  static constexpr int kBytesA = 128 * 128, kBytesB = BN * 128 / (PAIR ? 2 : 1), kBytesScales = 1024 * (1 + kScaleTiles);
   static constexpr int kBytes = kBytesA + kBytesB + kBytesScales;
   static constexpr int kRoom = kMxMostSmem - 1024 - kStagedBytes - 256;
   static constexpr int kStages = kRoom / kBytes < 6 ? kRoom / kBytes : 6;
@@ -154,11 +155,12 @@ struct MxTile {
 };
 
 struct MxParams {
-  const uint8_t *x_scales, *w_scales;
+  const uint8_t *x_scales, *w_scales;  // (pairs read them through tensor maps)
   const float* bias;
   int32_t* dev_status;
   int m_tiles, n_tiles, w_tiles;  // w_tiles: scale images along C_out
-  int C_out, chunks, steps;       // steps of 64 channels
+  int rows, C_out, chunks, steps; // steps of 64 channels
+  int x_rows, w_rows;             // of a tile's boxes: no more than there are (what lies past them is not stored)
   int tail_bytes;                 // of codes per row in the last stage's tiles: 32, 64 or 128
   uint32_t tail_desc;             // high half of their descriptors
 };
@@ -190,11 +192,33 @@ __device__ __forceinline__ void tc_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, ui
       ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(desc_hi)
       : "memory");
 }
+// The same two for a pair: both blocks' scales into their own TMEM; 256 rows of A, the blocks' halves of B one after the other.
+__device__ __forceinline__ void tc2_cp_32x128b_x4_w(uint32_t dst_tmem, uint32_t src_lo) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t.reg .b64 ds;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "mov.b64 ds, {%1, %2};\n\t"
+      "@e tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], ds;\n\t}"
+      ::"r"(dst_tmem), "r"(src_lo), "r"(kDescHiNoSwizzle128)
+      : "memory");
+}
+__device__ __forceinline__ void tc2_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
+                                               uint32_t sfb, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "mov.b64 da, {%1, %7};\n\t"
+      "mov.b64 db, {%2, %7};\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "@e tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(desc_hi)
+      : "memory");
+}
 // Instruction descriptor of kind::mxf4: bits 4-5 and 29-30 which of a row's scales in its TMEM word (0 or 2: the first two or the
 // last two) for B and A, bits 7-9 and 10-12 the formats (1 = e2m1), bits 17-22 N >> 3, bit 23 the scales' format (1 = e8m0),
 // bits 27-28 M >> 7.
-__host__ __device__ constexpr uint32_t make_idesc_mxf4(uint32_t N, uint32_t which) {
-  return (which << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (1u << 23) | (1u << 27) | (which << 29);
+__host__ __device__ constexpr uint32_t make_idesc_mxf4(uint32_t M, uint32_t N, uint32_t which) {
+  return (which << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (1u << 23) | ((M >> 7) << 27) | (which << 29);
 }
 // 16 columns of the warp's 32 lanes: register i of lane t holds column i of row t, after the wait below.
 __device__ __forceinline__ void tc_ld_32x32b_x16(uint32_t taddr, uint32_t (&r)[16]) {
@@ -215,13 +239,15 @@ __device__ __forceinline__ void tc_wait_ld_x16(uint32_t (&r)[16]) {
                : "memory");
 }
 
-template <int BN, int ACT>
-__global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __grid_constant__ CUtensorMap tm_x,
+template <int BN, bool PAIR, int ACT>
+__global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(const __grid_constant__ CUtensorMap tm_x,
                                                              const __grid_constant__ CUtensorMap tm_w,
                                                              const __grid_constant__ CUtensorMap tm_x_tail,
                                                              const __grid_constant__ CUtensorMap tm_w_tail,
+                                                             const __grid_constant__ CUtensorMap tm_x_scales,
+                                                             const __grid_constant__ CUtensorMap tm_w_scales,
                                                              const __grid_constant__ CUtensorMap tm_y, const MxParams p) {
-  using T = MxTile<BN>;
+  using T = MxTile<BN, PAIR>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* ring_a = smem;
@@ -229,7 +255,7 @@ __global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __
   uint8_t* staged = ring_b + T::kStages * T::kBytesB;
   uint8_t* ring_s = staged + T::kStagedBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring_s + T::kStages * T::kBytesScales);
-  uint64_t *full = bars, *empty = bars + T::kStages, *acc_full = bars + 2 * T::kStages, *acc_empty = acc_full + 2;
+  uint64_t *full = bars, *empty = bars + T::kStages, *scaled = bars + 2 * T::kStages, *acc_full = bars + 3 * T::kStages, *acc_empty = acc_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5;
@@ -239,10 +265,11 @@ __global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __
     for (int s = 0; s < T::kStages; ++s) {
       mbar_init(full + s, 1);
       mbar_init(empty + s, 1);
+      mbar_init(scaled + s, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(acc_full + i, 1);
-      mbar_init(acc_empty + i, 4 * kMxSets);
+      mbar_init(acc_empty + i, 4 * kMxSets * (PAIR ? 2 : 1));
     }
     *abort_flag = 0;
     mbar_fence_init();
@@ -255,41 +282,67 @@ __global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __
     prefetch_tensormap(&tm_y);
   }
   if (warp == T::kIssuer) {
-    tmem_alloc(tmem_slot, T::kTmem);
-    tmem_relinquish();
+    if (PAIR) {
+      tmem_alloc2(tmem_slot, T::kTmem);
+      tmem_relinquish2();
+    } else {
+      tmem_alloc(tmem_slot, T::kTmem);
+      tmem_relinquish();
+    }
   }
   tc_fence_before();
   __syncthreads();
+  if (PAIR) {  // (the other block's barriers are there too)
+    cluster_arrive();
+    cluster_wait();
+  }
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  // a pair: rank 0 leads; it issues the MMAs, and both blocks' copies arrive on its barriers
+  const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
+  const int first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x, tile_step = PAIR ? gridDim.x >> 1 : gridDim.x;
   grid_dependency_wait();
 
   const int tiles = p.m_tiles * p.n_tiles;
   const int stages = (p.steps + 3) >> 2;
   if (warp == T::kProducer) {
     // ---------------------------------------------------------------- producer
-    const uint32_t a0 = smem_u32(ring_a), b0 = smem_u32(ring_b), s0 = smem_u32(ring_s), full0 = smem_u32(full), empty0 = smem_u32(empty);
+    const uint32_t a0 = smem_u32(ring_a), b0 = smem_u32(ring_b), s0 = smem_u32(ring_s), empty0 = smem_u32(empty);
+    const uint32_t full0 = PAIR ? map_to_cta(smem_u32(full), 0) : smem_u32(full);
     uint32_t s = 0, phase = 0;
     bool ok = true;
-    for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-      const int m = t / p.n_tiles, n = t - m * p.n_tiles;
-      const uint8_t* xs = p.x_scales + (int64_t)m * p.chunks * kMxImageBytes;
+    for (int t = first_tile; t < tiles && ok; t += tile_step) {
+      const int mt = t / p.n_tiles, n = t - mt * p.n_tiles, m = PAIR ? 2 * mt + (int)rank : mt;
       const int first = n * BN >> 7;
       const int images = min((n * BN + BN - 1) >> 7, p.w_tiles - 1) - first + 1;
+      const uint8_t* xs = p.x_scales + (int64_t)m * p.chunks * kMxImageBytes;
+      const uint8_t* ws = p.w_scales + (int64_t)first * p.chunks * kMxImageBytes;
       for (int kb = 0; kb < stages; ++kb) {
         if (!mbar_wait_warp_a(empty0 + 8 * s, phase ^ 1u, abort_flag, kMxWaitLimit)) {
           ok = false;
           break;
         }
         const uint32_t bar = full0 + 8 * s, sc = s0 + s * T::kBytesScales;
-        const uint32_t part = min(2, p.chunks - 2 * kb) * kMxImageBytes;
         const bool tail = kb == stages - 1;
-        mbar_expect_tx_w(bar, (tail ? p.tail_bytes : 128) * (128 + BN) + part * (1 + images));
-        tma_load_2d_w(a0 + s * T::kBytesA, tail ? &tm_x_tail : &tm_x, bar, kb * 128, m * 128);
-        tma_load_2d_w(b0 + s * T::kBytesB, tail ? &tm_w_tail : &tm_w, bar, kb * 128, n * BN);
-        bulk_load_w(sc, xs + kb * 2 * kMxImageBytes, part, bar);
-        for (int i = 0; i < images; ++i)
-          bulk_load_w(sc + 1024 * (1 + i), p.w_scales + ((int64_t)(first + i) * p.chunks + 2 * kb) * kMxImageBytes, part, bar);
+        const uint32_t codes = (tail ? p.tail_bytes : 128) * (p.x_rows + p.w_rows);
+        if constexpr (PAIR) {
+          // (two images per copy, whether there is a second one or not: what it brings instead is not used)
+          if (rank == 0) mbar_expect_tx_w(smem_u32(full) + 8 * s, 2 * (codes + T::kBytesScales));
+          tma2_load_2d_w(a0 + s * T::kBytesA, tail ? &tm_x_tail : &tm_x, bar, kb * 128, m * 128);
+          tma2_load_2d_w(b0 + s * T::kBytesB, tail ? &tm_w_tail : &tm_w, bar, kb * 128, n * BN + (int)rank * (BN / 2));
+          tma2_load_2d_w(sc, &tm_x_scales, bar, 0, m * p.chunks + 2 * kb);
+#pragma unroll
+          for (int i = 0; i < T::kScaleTiles; ++i) tma2_load_2d_w(sc + 1024 * (1 + i), &tm_w_scales, bar, 0, (first + i) * p.chunks + 2 * kb);
+        } else {
+          const uint32_t part = min(2, p.chunks - 2 * kb) * kMxImageBytes;
+          mbar_expect_tx_w(bar, codes + part * (1 + images));
+          tma_load_2d_w(a0 + s * T::kBytesA, tail ? &tm_x_tail : &tm_x, bar, kb * 128, m * 128);
+          tma_load_2d_w(b0 + s * T::kBytesB, tail ? &tm_w_tail : &tm_w, bar, kb * 128, n * BN);
+          bulk_load_w(sc, xs + kb * 2 * kMxImageBytes, part, bar);
+#pragma unroll
+          for (int i = 0; i < T::kScaleTiles; ++i)
+            if (i < images) bulk_load_w(sc + 1024 * (1 + i), ws + ((int64_t)i * p.chunks + 2 * kb) * kMxImageBytes, part, bar);
+        }
         if (++s == T::kStages) {
           s = 0;
           phase ^= 1u;
@@ -297,54 +350,106 @@ __global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __
       }
     }
   } else if (warp == T::kIssuer) {
+   if (rank == 0) {
     // ---------------------------------------------------------------- MMA issuer
-    const uint32_t a0 = desc_lo(smem_u32(ring_a)), b0 = desc_lo(smem_u32(ring_b)), s0 = desc_lo(smem_u32(ring_s));
-    const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
-    uint32_t s = 0, phase = 0, buf = 0, acc_phase = 0;
+    const uint32_t a0 = desc_lo(smem_u32(ring_a)), b0 = desc_lo(smem_u32(ring_b));
+    const uint32_t scaled0 = smem_u32(scaled), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
+    uint32_t s = 0, phase = 0, buf = 0, acc_phase = 0, ready = 0;
     bool ok = true;
-    for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+    for (int t = first_tile; t < tiles && ok; t += tile_step) {
       // tiles that start inside an image take its later columns
       const uint32_t shift = ((uint32_t)(t % p.n_tiles) * BN & 127u) >> 5;
       if (!mbar_wait_warp_a(acc_empty0 + 8 * buf, acc_phase ^ 1u, abort_flag, kMxWaitLimit)) break;
       tc_fence_after();
       const uint32_t d = tmem + buf * BN;
       for (int kb = 0; kb < stages; ++kb) {
-        if (!mbar_wait_warp_a(full0 + 8 * s, phase, abort_flag, kMxWaitLimit)) {
+        if (!__all_sync(0xFFFFFFFFu, ready) && !mbar_wait_warp_a(scaled0 + 8 * s, phase, abort_flag, kMxWaitLimit)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        const uint32_t sfa = tmem + 2 * BN + s * T::kScaleColumns, sfb = sfa + 8;
-        const uint32_t src = s0 + s * (T::kBytesScales >> 4);
+        const uint32_t next = s + 1 == T::kStages ? 0 : s + 1, next_phase = next == 0 ? phase ^ 1u : phase;
+        ready = mbar_test_a(scaled0 + 8 * next, next_phase);  // (its latency passes beside the MMAs)
+        const uint32_t sfa = tmem + 2 * BN + s * T::kScaleColumns, sfb = sfa + 8 + shift;
         const int steps = min(4, p.steps - 4 * kb);
         const uint32_t desc_hi = kb == stages - 1 ? p.tail_desc : kDescHiSw128;
-        for (int c = 0; 2 * c < steps; ++c) {
-          tc_cp_32x128b_x4_w(sfa + 4 * c, src + 32 * c);
+        const uint32_t a_lo = a0 + s * (T::kBytesA >> 4), b_lo = b0 + s * (T::kBytesB >> 4);
 #pragma unroll
-          for (int i = 0; i < T::kScaleTiles; ++i) tc_cp_32x128b_x4_w(sfb + 4 * T::kScaleTiles * c + 4 * i, src + 64 * (1 + i) + 32 * c);
-        }
-        for (int k = 0; k < steps; ++k)
-          tc_mma_mxf4_w(d, a0 + s * (T::kBytesA >> 4) + 2 * k, b0 + s * (T::kBytesB >> 4) + 2 * k, desc_hi,
-                        make_idesc_mxf4(BN, 2 * (k & 1)), sfa + 4 * (k >> 1), sfb + 4 * T::kScaleTiles * (k >> 1) + shift, (kb | k) != 0);
-        tc_commit_w(empty0 + 8 * s);
-        if (++s == T::kStages) {
-          s = 0;
-          phase ^= 1u;
-        }
+        for (int k = 0; k < 4; ++k)
+          if (k < steps) {
+            const uint32_t idesc = make_idesc_mxf4(PAIR ? 256 : 128, BN, 2 * (k & 1));
+            const uint32_t sa = sfa + 4 * (k >> 1), sb = sfb + 4 * T::kScaleTiles * (k >> 1);
+            if (PAIR)
+              tc2_mma_mxf4_w(d, a_lo + 2 * k, b_lo + 2 * k, desc_hi, idesc, sa, sb, (kb | k) != 0);
+            else
+              tc_mma_mxf4_w(d, a_lo + 2 * k, b_lo + 2 * k, desc_hi, idesc, sa, sb, (kb | k) != 0);
+          }
+        if (PAIR)
+          tc2_commit_both_w(empty0 + 8 * s);
+        else
+          tc_commit_w(empty0 + 8 * s);
+        s = next;
+        phase = next_phase;
       }
       if (!ok) break;
-      tc_commit_w(acc_full0 + 8 * buf);
+      if (PAIR)
+        tc2_commit_both_w(acc_full0 + 8 * buf);
+      else
+        tc_commit_w(acc_full0 + 8 * buf);
       buf ^= 1u;
       if (buf == 0) acc_phase ^= 1u;
     }
+   }
+  } else if (warp == T::kScaler) {
+   if (rank == 0) {
+    // ---------------------------------------------------------------- scales into TMEM
+    // (by a warp of its own: an issuer takes some 60 cycles per tcgen05 instruction and 200 per wait, and there are six of these
+    // beside four MMAs)
+    const uint32_t s0 = desc_lo(smem_u32(ring_s)), full0 = smem_u32(full), scaled0 = smem_u32(scaled);
+    uint32_t s = 0, phase = 0, ready = 0;
+    bool ok = true;
+    for (int t = first_tile; t < tiles && ok; t += tile_step) {
+      for (int kb = 0; kb < stages; ++kb) {
+        if (!__all_sync(0xFFFFFFFFu, ready) && !mbar_wait_warp_a(full0 + 8 * s, phase, abort_flag, kMxWaitLimit)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t next = s + 1 == T::kStages ? 0 : s + 1, next_phase = next == 0 ? phase ^ 1u : phase;
+        ready = mbar_test_a(full0 + 8 * next, next_phase);
+        const uint32_t sfa = tmem + 2 * BN + s * T::kScaleColumns, sfb = sfa + 8, src = s0 + s * (T::kBytesScales >> 4);
+        const bool second = p.steps - 4 * kb > 2;
+        const auto copy = [](uint32_t to, uint32_t from) {
+          if (PAIR)
+            tc2_cp_32x128b_x4_w(to, from);
+          else
+            tc_cp_32x128b_x4_w(to, from);
+        };
+        copy(sfa, src);
+#pragma unroll
+        for (int i = 0; i < T::kScaleTiles; ++i) copy(sfb + 4 * i, src + 64 * (1 + i));
+        if (second) {
+          copy(sfa + 4, src + 32);
+#pragma unroll
+          for (int i = 0; i < T::kScaleTiles; ++i) copy(sfb + 4 * T::kScaleTiles + 4 * i, src + 64 * (1 + i) + 32);
+        }
+        if (PAIR)
+          tc2_commit_w(map_to_cta(scaled0 + 8 * s, 0));
+        else
+          tc_commit_w(scaled0 + 8 * s);
+        s = next;
+        phase = next_phase;
+      }
+    }
+   }
   } else {
     // ---------------------------------------------------------------- epilogue
     const int set = warp >> 2, row = 32 * (warp & 3), lane = threadIdx.x & 31;
     uint8_t* out = staged + warp * kMxStoreBytes;
     uint32_t buf = 0, acc_phase = 0;
     int turn = 0;  // the set that takes the next piece
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-      const int m = t / p.n_tiles, n = t - m * p.n_tiles;
+    for (int t = first_tile; t < tiles; t += tile_step) {
+      const int mt = t / p.n_tiles, n = t - mt * p.n_tiles, m = PAIR ? 2 * mt + (int)rank : mt;
       if (!mbar_wait_warp(acc_full + buf, acc_phase, abort_flag, kMxWaitLimit)) break;
       tc_fence_after();
       const uint32_t acc = tmem + buf * BN + ((uint32_t)row << 16);
@@ -355,10 +460,11 @@ __global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __
         const bool mine = turn == set;
         turn = turn + 1 == kMxSets ? 0 : turn + 1;
         if (!mine) continue;
-        // a row's 64 outputs per lane, computed while the warp's last piece leaves its buffer; the next 16 columns are on their way
-        uint4 o[8];
+        // a row's 64 outputs per lane; the next 16 columns are on their way
         uint32_t r[2][16];
         tc_ld_32x32b_x16(acc + 64 * g, r[0]);
+        if (lane == 0) bulk_wait_group_read0();  // the warp's last piece has left its buffer
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           ulonglong2 bias[4];
@@ -382,23 +488,24 @@ __global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __
             split2(v, lo, hi);
             w[j] = activate_pack<ACT>(lo, hi);
           }
-          o[2 * i] = make_uint4(w[0], w[1], w[2], w[3]);
-          o[2 * i + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+          *reinterpret_cast<uint4*>(out + lane * 128 + (((2 * i) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(out + lane * 128 + (((2 * i + 1) ^ (lane & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
         }
-        if (lane == 0) bulk_wait_group_read0();
-        __syncwarp();
-#pragma unroll
-        for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(out + lane * 128 + ((q ^ (lane & 7)) << 4)) = o[q];
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          tma_store_2d(&tm_y, out, c0, m * 128 + row);
+          if (!PAIR || m * 128 + row < p.rows) tma_store_2d(&tm_y, out, c0, m * 128 + row);
           bulk_commit_group();
         }
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(acc_empty + buf);
+      if (lane == 0) {
+        if (PAIR)
+          mbar_arrive_cluster(map_to_cta(smem_u32(acc_empty + buf), 0));
+        else
+          mbar_arrive(acc_empty + buf);
+      }
       buf ^= 1u;
       if (buf == 0) acc_phase ^= 1u;
     }
@@ -414,9 +521,16 @@ __global__ void __launch_bounds__(MxTile<BN>::kThreads, 1) mxfp4_kernel(const __
     if (threadIdx.x == 0 && p.dev_status != nullptr) atomicExch(p.dev_status, (int)SSCONV_ERR_TIMEOUT);
     __syncthreads();
   }
+  if (PAIR) {  // (neither block leaves while the other may still arrive on its barriers or read its memory)
+    cluster_arrive();
+    cluster_wait();
+  }
   if (warp == T::kIssuer) {
     tc_fence_after();
-    tmem_dealloc(tmem, T::kTmem);
+    if (PAIR)
+      tmem_dealloc2(tmem, T::kTmem);
+    else
+      tmem_dealloc(tmem, T::kTmem);
   }
 }
 
@@ -453,11 +567,56 @@ bool encode_matrix(EncodeFn f, CUtensorMap* map, CUtensorMapDataType type, int e
            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-using MxKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, MxParams);
-template <int BN>
+// Scale images, two per copy, unswizzled.
+bool encode_images(EncodeFn f, CUtensorMap* map, const void* base, int64_t images) {
+  const cuuint64_t dims[2] = {kMxImageBytes / 4, (cuuint64_t)images}, strides[1] = {kMxImageBytes};
+  const cuuint32_t box[2] = {kMxImageBytes / 4, 2}, ones[2] = {1, 1};
+  return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+using MxKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, MxParams);
+template <int BN, bool PAIR>
 MxKernel mx_kernel(int act, int* smem) {
-  *smem = MxTile<BN>::kSmem;
-  return act == kActGelu ? mxfp4_kernel<BN, kActGelu> : act == kActRelu ? mxfp4_kernel<BN, kActRelu> : mxfp4_kernel<BN, kActNone>;
+  *smem = MxTile<BN, PAIR>::kSmem;
+  return act == kActGelu ? mxfp4_kernel<BN, PAIR, kActGelu> : act == kActRelu ? mxfp4_kernel<BN, PAIR, kActRelu> : mxfp4_kernel<BN, PAIR, kActNone>;
+}
+constexpr int kMxThreads = MxTile<64, false>::kThreads;
+
+cudaLaunchConfig_t mx_config(unsigned blocks, int smem, bool pair, cudaStream_t st, cudaLaunchAttribute (&attrs)[2]) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = blocks;
+  cfg.blockDim = kMxThreads;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = 2;
+  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+  cfg.attrs = attrs;
+  cfg.numAttrs = pair ? 2 : 1;
+  return cfg;
+}
+
+// Checks a device and allows the kernels their shared memory on it, once; the pairs of blocks that it holds at a time.
+int32_t mx_device(int dev, int* pairs) {
+  static std::atomic<int> known[64];
+  *pairs = known[dev].load(std::memory_order_acquire);
+  if (*pairs > 0) return SSCONV_OK;
+  int major = 0, smem = 0;
+  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return SSCONV_ERR_CUDA;
+  if (major != 10) return SSCONV_ERR_ARCH;
+  for (const int act : {kActNone, kActRelu, kActGelu})
+    for (const MxKernel kernel : {mx_kernel<64, false>(act, &smem), mx_kernel<128, false>(act, &smem), mx_kernel<192, false>(act, &smem),
+                                  mx_kernel<192, true>(act, &smem)})
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxMostSmem) != cudaSuccess) return SSCONV_ERR_CUDA;
+  cudaLaunchAttribute attrs[2];
+  const MxKernel kernel = mx_kernel<192, true>(kActNone, &smem);
+  const cudaLaunchConfig_t cfg = mx_config(2u * device_sms(), smem, true, nullptr, attrs);
+  if (cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg) != cudaSuccess || *pairs <= 0) return SSCONV_ERR_CUDA;
+  known[dev].store(*pairs, std::memory_order_release);
+  return SSCONV_OK;
 }
 
 }  // namespace
@@ -480,61 +639,84 @@ int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const 
                              const float* bias, void* y, int32_t* dev_status, cudaStream_t st) {
   const int64_t rows = (int64_t)d.N * d.H * d.W;
   const MxGeometry gx = mx_geometry(rows, d.C_in), gw = mx_geometry(d.C_out, d.C_in);
-  // The width that keeps the SMs busy: a tile costs its columns and a fixed part.
-  int dev = 0, major = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess)
-    return SSCONV_ERR_CUDA;
-  if (major != 10) return SSCONV_ERR_ARCH;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SSCONV_ERR_CUDA;
+  int pairs = 0;
+  const int32_t known = mx_device(dev, &pairs);
+  if (known != SSCONV_OK) return known;
   const int sms = device_sms();
+  const int act = activation_of(d.flags);
+  // The width, by cycles (fitted to 401408 x 96 -> 384 at the three widths and 8192 x 4096 -> 4096): a tile takes the longer of
+  // filling shared memory (50 bytes per cycle) and of its epilogue, and the first of the one and the last of the other are not hidden.
+  // us at 192 / 128 / 64 columns: 401408 x 96 -> 384 73 / 77 / 92, 8192 x 4096 -> 4096 87 / 113 / 215, 3136 x 256 -> 1024 8.1 / 6.3 / 8.3.
+  const int mx_stages = (gx.blocks + 7) / 8;
   int bn = 0;
-  int64_t least = 0;
-  for (const int w : {192, 128, 64}) {
-    const int64_t tiles = gx.row_tiles * ((d.C_out + w - 1) / w);
-    const int64_t cost = (tiles + sms - 1) / sms * (w + 32);
-    if (bn == 0 || cost < least) {
+  bool pair = false;
+  double least = 0.0;
+  const auto consider = [&](int w, bool two) {
+    const int64_t rows_of_tiles = two ? (gx.row_tiles + 1) / 2 : gx.row_tiles, at_once = two ? pairs : sms;
+    const int64_t turns = (rows_of_tiles * ((d.C_out + w - 1) / w) + at_once - 1) / at_once;
+    const double fill = mx_stages * (128 + (two ? w / 2 + 16 : w) + 8) * 128 / 50.0, epilogue = 800.0 + w * (act == kActGelu ? 19.0 : 14.0);
+    const double cost = turns * (fill > epilogue ? fill : epilogue) + (fill > epilogue ? epilogue : fill);
+    if (bn == 0 || cost < 0.9 * least) {
       bn = w;
+      pair = two;
       least = cost;
     }
-  }
+  };
+  consider(192, false);
+  consider(128, false);
+  consider(64, false);
+  consider(192, true);
   int smem = 0;
-  const int act = activation_of(d.flags);
-  const MxKernel kernel = bn == 192 ? mx_kernel<192>(act, &smem) : bn == 128 ? mx_kernel<128>(act, &smem) : mx_kernel<64>(act, &smem);
+  const MxKernel kernel = pair        ? mx_kernel<192, true>(act, &smem)
+                          : bn == 192 ? mx_kernel<192, false>(act, &smem)
+                          : bn == 128 ? mx_kernel<128, false>(act, &smem)
+                                      : mx_kernel<64, false>(act, &smem);
   const int64_t row_bytes = (int64_t)gx.blocks * 16;
   MxParams p = {};
   p.x_scales = static_cast<const uint8_t*>(x_scales);
   p.w_scales = static_cast<const uint8_t*>(w_scales);
   p.bias = (d.flags & SSCONV_FLAG_BIAS) ? bias : nullptr;
   p.dev_status = dev_status;
-  p.m_tiles = (int)gx.row_tiles;
+  p.rows = (int)rows;
+  p.m_tiles = (int)(pair ? (gx.row_tiles + 1) / 2 : gx.row_tiles);
   p.n_tiles = (d.C_out + bn - 1) / bn;
   p.w_tiles = (int)gw.row_tiles;
   p.C_out = d.C_out;
   p.chunks = gx.chunks;
   p.steps = (gx.blocks + 1) / 2;
   const int tail = (int)((row_bytes - 1) % 128 + 1), stages = (p.steps + 3) / 4;
+  p.x_rows = (int)(rows < 128 ? (rows + 7) / 8 * 8 : 128);
+  p.w_rows = pair ? bn / 2 : d.C_out < bn ? d.C_out : bn;
+  if (pair) p.x_rows = 128;
   p.tail_bytes = tail <= 32 ? 32 : tail <= 64 ? 64 : 128;
   p.tail_desc = tail <= 32 ? kDescHiSw32 : tail <= 64 ? kDescHiSw64 : kDescHiSw128;
   const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
   if (tiles > 0x7FFFFFFF - 4096) return SSCONV_ERR_UNSUPPORTED_SHAPE;
   const EncodeFn encode = encoder();
   if (encode == nullptr) return SSCONV_ERR_CUDA;
-  CUtensorMap tm_x, tm_w, tm_x_tail, tm_w_tail, tm_y;
+  CUtensorMap tm_x, tm_w, tm_x_tail, tm_w_tail, tm_x_scales, tm_w_scales, tm_y;
   const auto codes = [&](CUtensorMap* map, const void* base, int64_t n, int width, int box_rows) {
     return encode_matrix(encode, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, row_bytes, n, width, box_rows);
   };
-  if (!codes(&tm_x_tail, x_codes, rows, p.tail_bytes, 128) || !codes(&tm_w_tail, w_codes, d.C_out, p.tail_bytes, bn) ||
+  if (!codes(&tm_x_tail, x_codes, rows, p.tail_bytes, p.x_rows) || !codes(&tm_w_tail, w_codes, d.C_out, p.tail_bytes, p.w_rows) ||
       !encode_matrix(encode, &tm_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, y, d.C_out, rows, 128, 32))
     return SSCONV_ERR_CUDA;
   tm_x = tm_x_tail;
   tm_w = tm_w_tail;
-  if (stages > 1 && p.tail_bytes != 128 && (!codes(&tm_x, x_codes, rows, 128, 128) || !codes(&tm_w, w_codes, d.C_out, 128, bn)))
+  if (stages > 1 && p.tail_bytes != 128 && (!codes(&tm_x, x_codes, rows, 128, p.x_rows) || !codes(&tm_w, w_codes, d.C_out, 128, p.w_rows)))
     return SSCONV_ERR_CUDA;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SSCONV_ERR_CUDA;
+  tm_x_scales = tm_w_scales = tm_y;  // (not used without pairs)
+  if (pair && (!encode_images(encode, &tm_x_scales, x_scales, gx.row_tiles * gx.chunks) || !encode_images(encode, &tm_w_scales, w_scales, gw.row_tiles * gw.chunks)))
+    return SSCONV_ERR_CUDA;
+  const int64_t at_once = pair ? pairs : sms;
+  const unsigned blocks = (unsigned)((tiles < at_once ? tiles : at_once) * (pair ? 2 : 1));
+  cudaLaunchAttribute attrs[2];
+  const cudaLaunchConfig_t cfg = mx_config(blocks, smem, pair, st, attrs);
   count_launch();
-  return launch_dependent_smem(kernel, (unsigned)(tiles < sms ? tiles : sms), MxTile<64>::kThreads, smem, st, tm_x, tm_w, tm_x_tail, tm_w_tail, tm_y, p) ==
-                 cudaSuccess
-             ? SSCONV_OK
-             : SSCONV_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, kernel, tm_x, tm_w, tm_x_tail, tm_w_tail, tm_x_scales, tm_w_scales, tm_y, p) == cudaSuccess ? SSCONV_OK
+                                                                                                                            : SSCONV_ERR_CUDA;
 }
 
 }  // namespace ssconv
