@@ -17,8 +17,9 @@ namespace {
 // Quantisation.  The scale's exponent comes from the exponent field E of the block's largest magnitude: floor(log2) = E - 127, so
 // the code (bias 127) is E - 2, at least 0; E = 255 (an infinity or a NaN) gives 255.  Elements are multiplied by the inverse
 // power of two (exact) and rounded once.  A thread block takes the 128 rows x 128 channels of a scale image, 16 lanes a row and
-// four lanes a block of 32, each thread eight rows: eight loads in flight, and the image is written whole.  DRAM-bound: 2.53
-// bytes per element.
+// four lanes a block of 32, each thread four rows: four loads in flight, and the image is written whole.  2.53 bytes per element;
+// 401408 x 96 in 22.9 us (4.3 TB/s; a quarter of the lanes have no channels there, and conversions and shuffles take their share),
+// 25088 x 1536 in 20.
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -47,9 +48,9 @@ __device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, uint32_t scale_x2) {
   return out;
 }
 
-constexpr int kMxRowsPerThread = 8;  // 16 rows of threads
+constexpr int kMxQuantThreads = 512, kMxRowsPerThread = 4;  // 32 rows of threads
 
-__global__ void __launch_bounds__(256) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint4* scales, uint32_t rows, uint32_t chunks,
+__global__ void __launch_bounds__(kMxQuantThreads) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint4* scales, uint32_t rows, uint32_t chunks,
                                                              uint32_t blocks, uint32_t C8) {
   __shared__ __align__(16) uint32_t image[128];
   grid_launch_dependents();
@@ -61,13 +62,13 @@ __global__ void __launch_bounds__(256) quantize_mxfp4_kernel(const uint4* x, uin
   uint4 v[kMxRowsPerThread];
 #pragma unroll
   for (int u = 0; u < kMxRowsPerThread; ++u) {
-    const uint32_t r = r0 + 16u * u;
+    const uint32_t r = r0 + 32u * u;
     v[u] = make_uint4(0u, 0u, 0u, 0u);
     if (r < there && piece < C8) v[u] = x[(uint64_t)(tile * 128u + r) * C8 + piece];
   }
 #pragma unroll
   for (int u = 0; u < kMxRowsPerThread; ++u) {
-    const uint32_t r = r0 + 16u * u;
+    const uint32_t r = r0 + 32u * u;
     constexpr uint32_t kMagnitudes = 0x7FFF7FFFu;
     uint32_t m = max_bf16x2(max_bf16x2(v[u].x & kMagnitudes, v[u].y & kMagnitudes), max_bf16x2(v[u].z & kMagnitudes, v[u].w & kMagnitudes));
     m = max_bf16x2(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
@@ -93,7 +94,7 @@ __device__ __forceinline__ void e2m1_values_x4(uint32_t codes, uint32_t& low, ui
   low = __byte_perm(lo, hi, 0x5140) | ((codes << 12) & 0x8000u) | ((codes << 24) & 0x80000000u);
   high = __byte_perm(lo, hi, 0x7362) | ((codes << 4) & 0x8000u) | ((codes << 16) & 0x80000000u);
 }
-__global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint32_t rows, uint32_t chunks,
+__global__ void __launch_bounds__(kMxQuantThreads) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint32_t rows, uint32_t chunks,
                                                                uint32_t blocks, uint32_t C8) {
   grid_launch_dependents();
   const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* c
   uint32_t c[kMxRowsPerThread], s[kMxRowsPerThread];
 #pragma unroll
   for (int u = 0; u < kMxRowsPerThread; ++u) {
-    const uint32_t r = r0 + 16u * u;
+    const uint32_t r = r0 + 32u * u;
     c[u] = s[u] = 0u;
     if (r < there) {
       c[u] = codes[(uint64_t)(tile * 128u + r) * (4u * blocks) + piece];
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(256) dequantize_mxfp4_kernel(const uint32_t* c
   }
 #pragma unroll
   for (int u = 0; u < kMxRowsPerThread; ++u) {
-    const uint32_t r = r0 + 16u * u;
+    const uint32_t r = r0 + 32u * u;
     // the scale as bf16: 2^-127 is below the normal numbers, 255 is a NaN
     const uint32_t scale = (s[u] == 255u ? 0x7FC0u : s[u] == 0u ? 0x0040u : s[u] << 7) * 0x10001u;
     uint4 o;
@@ -624,14 +625,14 @@ int32_t mx_device(int dev, int* pairs) {
 cudaError_t launch_quantize_mxfp4(const void* x, int64_t rows, int C, void* codes, void* scales, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
   count_launch();
-  return launch_dependent(quantize_mxfp4_kernel, (unsigned)(g.row_tiles * g.chunks), 256, st, (const uint4*)x, (uint32_t*)codes, (uint4*)scales,
+  return launch_dependent(quantize_mxfp4_kernel, (unsigned)(g.row_tiles * g.chunks), kMxQuantThreads, st, (const uint4*)x, (uint32_t*)codes, (uint4*)scales,
                           (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
 cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int C, void* x, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
   count_launch();
-  return launch_dependent(dequantize_mxfp4_kernel, (unsigned)(g.row_tiles * g.chunks), 256, st, (const uint32_t*)codes, (const uint8_t*)scales,
+  return launch_dependent(dequantize_mxfp4_kernel, (unsigned)(g.row_tiles * g.chunks), kMxQuantThreads, st, (const uint32_t*)codes, (const uint8_t*)scales,
                           (uint4*)x, (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
@@ -646,9 +647,11 @@ int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const 
   if (known != SSCONV_OK) return known;
   const int sms = device_sms();
   const int act = activation_of(d.flags);
-  // The width, by cycles (fitted to 401408 x 96 -> 384 at the three widths and 8192 x 4096 -> 4096): a tile takes the longer of
-  // filling shared memory (50 bytes per cycle) and of its epilogue, and the first of the one and the last of the other are not hidden.
-  // us at 192 / 128 / 64 columns: 401408 x 96 -> 384 73 / 77 / 92, 8192 x 4096 -> 4096 87 / 113 / 215, 3136 x 256 -> 1024 8.1 / 6.3 / 8.3.
+  // The width, by cycles (fitted to 401408 x 96 -> 384 and 8192 x 4096 -> 4096): a tile takes the longer of filling shared memory and
+  // of its epilogue, and the first of the one and the last of the other are not hidden.  Shared memory fills at 50 bytes per cycle and
+  // SM, 12 TB/s out of L2 in all, which is what long K is bound by (with three of four MMAs left out 8192 x 4096 -> 4096 still took 62 us
+  // of 72).  Pairs halve the weights' share of it, at a lower rate.  us at 192 / 128 / 64 columns / 192 on pairs: 401408 x 96 -> 384 74 /
+  // 76 / 93, 8192 x 4096 -> 4096 77 / 90 / 162 / 72, 25088 x 1536 -> 384 14.4 / 16.4 / 24.7 / 15.1, 3136 x 256 -> 1024 8.1 / 6.3 / 8.3.
   const int mx_stages = (gx.blocks + 7) / 8;
   int bn = 0;
   bool pair = false;
@@ -656,9 +659,9 @@ int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const 
   const auto consider = [&](int w, bool two) {
     const int64_t rows_of_tiles = two ? (gx.row_tiles + 1) / 2 : gx.row_tiles, at_once = two ? pairs : sms;
     const int64_t turns = (rows_of_tiles * ((d.C_out + w - 1) / w) + at_once - 1) / at_once;
-    const double fill = mx_stages * (128 + (two ? w / 2 + 16 : w) + 8) * 128 / 50.0, epilogue = 800.0 + w * (act == kActGelu ? 19.0 : 14.0);
+    const double fill = mx_stages * (two ? 790.0 : (128 + w + 8) * 128 / 50.0), epilogue = 800.0 + w * (act == kActGelu ? 19.0 : 14.0);
     const double cost = turns * (fill > epilogue ? fill : epilogue) + (fill > epilogue ? epilogue : fill);
-    if (bn == 0 || cost < 0.9 * least) {
+    if (bn == 0 || cost < (two ? 0.95 : 0.9) * least) {
       bn = w;
       pair = two;
       least = cost;
