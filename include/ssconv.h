@@ -524,7 +524,8 @@ int32_t ssconv_adamw_multi(void* const* theta, const void* const* g, void* const
  * or SSCONV_NORM_RMS (v / sqrt(mean(v^2) + eps) * gamma + beta).  gamma, beta: fp32 [C], NULL for ones and zeros.  gate: fp32,
  * NULL (ones), [C] with rows_per_gate = 0, or [ceil(rows / rows_per_gate)][C]: row r takes gates r / rows_per_gate.  x, b, h, y: bf16
  * [rows][C]; arithmetic in fp32, y is the norm of h before h is rounded.  stats (nullable): fp32 [rows][4], what the backward call
- * needs of both norms (mean and 1/deviation of b, then of h).  h (nullable if y is wanted) and y may be the buffer of x or of b.
+ * needs of both norms (mean and 1/deviation of b, then of h).  h (nullable if y is wanted) and y may be the buffer of x or of b
+ * (overlapping them in another way, or each other, is SSCONV_ERR_BAD_DESC).
  * C % 8 == 0, C <= 8192, rows <= 2^30 (rows = 0 is a no-op); tensors 16-byte aligned. */
 enum { SSCONV_NORM_NONE = 0, SSCONV_NORM_LAYER = 1, SSCONV_NORM_RMS = 2 };
 typedef struct {
@@ -539,8 +540,8 @@ int32_t ssconv_residual_norm(const ssconv_resnorm_t* desc, const void* x, const 
  * [rows][C]; dgate of the shape of gate; dpost_gamma, dpost_beta, dpre_gamma, dpre_beta fp32 [C]: sums over rows in fp32, in a fixed
  * order.  Any output may be NULL (not computed); those of a norm that is not there must be.  stats: as the forward call wrote them
  * (ignored without norms).  rows = 0 writes zeros to dgate (if shared) and to the gradients of the norms' parameters.  ws: device
- * scratch of ssconv_residual_norm_ws_bytes bytes, 16-byte aligned, that no other call in flight uses.  Outputs must not overlap
- * inputs. */
+ * scratch of ssconv_residual_norm_ws_bytes bytes, 16-byte aligned, that no other call in flight uses.  dx and db must not overlap
+ * inputs or each other (SSCONV_ERR_BAD_DESC). */
 int32_t ssconv_residual_norm_ws_bytes(const ssconv_resnorm_t* desc, size_t* bytes);
 int32_t ssconv_residual_norm_backward(const ssconv_resnorm_t* desc, const void* x, const void* b, const float* stats,
                                       const void* dh, const void* dy, const float* gate, const float* post_gamma,

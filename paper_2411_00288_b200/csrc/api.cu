@@ -193,6 +193,13 @@ bool written_once(std::vector<Span>& spans) {
   return true;
 }
 
+// Whether two buffers of that many bytes share memory without being the same one.
+bool overlap_partly(const void* a, const void* b, size_t bytes) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  return a && b && p != q && p < q + bytes && q < p + bytes;
+}
+bool overlap(const void* a, const void* b, size_t bytes) { return a && (a == b || overlap_partly(a, b, bytes)); }
+
 int32_t check_resnorm(const ssconv_resnorm_t* d) {
   if (!d) return SSCONV_ERR_NULL;
   if (d->rows < 0 || d->rows_per_gate < 0 || d->C <= 0 || !(d->eps >= 0.0f) || !std::isfinite(d->eps) || !std::isfinite(d->scale))
@@ -1171,10 +1178,13 @@ int32_t ssconv_residual_norm(const ssconv_resnorm_t* desc, const void* x, const 
   if (desc->rows == 0) return SSCONV_OK;
   if (!x || !b || (!h && !y) || (desc->pre != SSCONV_NORM_NONE && !y)) return SSCONV_ERR_NULL;
   if (desc->pre == SSCONV_NORM_NONE && y) return SSCONV_ERR_BAD_DESC;
-  if (h && h == y) return SSCONV_ERR_BAD_DESC;
   for (const void* p : {x, b, (const void*)gate, (const void*)post_gamma, (const void*)post_beta, (const void*)pre_gamma, (const void*)pre_beta,
                         (const void*)h, (const void*)y, (const void*)stats})
     if (!aligned16(p)) return SSCONV_ERR_ALIGNMENT;
+  const size_t bytes = 2 * (size_t)desc->rows * desc->C;
+  if (overlap(h, y, bytes)) return SSCONV_ERR_BAD_DESC;
+  for (const void* in : {x, b})
+    if (overlap_partly(h, in, bytes) || overlap_partly(y, in, bytes)) return SSCONV_ERR_BAD_DESC;
   return ssconv::launch_resnorm(*desc, {x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, h, y, stats}, (cudaStream_t)stream) == cudaSuccess
              ? SSCONV_OK
              : SSCONV_ERR_CUDA;
@@ -1206,6 +1216,10 @@ int32_t ssconv_residual_norm_backward(const ssconv_resnorm_t* desc, const void* 
     return SSCONV_OK;
   }
   if (!x || !b || ((post || pre) && !stats) || (pre && !dy) || (!pre && !dh)) return SSCONV_ERR_NULL;
+  const size_t bytes = 2 * (size_t)desc->rows * desc->C;
+  if (overlap(dx, db, bytes)) return SSCONV_ERR_BAD_DESC;
+  for (const void* in : {x, b, dh, dy})
+    if (overlap(dx, in, bytes) || overlap(db, in, bytes)) return SSCONV_ERR_BAD_DESC;
   if (!ws || ws_bytes < ssconv::resnorm_scratch(*desc)) return SSCONV_ERR_WORKSPACE;
   return ssconv::launch_resnorm_backward(*desc, {x, b, gate, post_gamma, post_beta, pre_gamma, nullptr, nullptr, nullptr, const_cast<float*>(stats)},
                                          {dh, dy, dx, db, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta}, static_cast<float*>(ws),

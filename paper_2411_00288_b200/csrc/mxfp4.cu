@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, uint32_t scale_x2) {
 
 constexpr int kMxQuantThreads = 512, kMxRowsPerThread = 4;  // 32 rows of threads
 
-__global__ void __launch_bounds__(kMxQuantThreads) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint4* scales, uint32_t rows, uint32_t chunks,
+__global__ void __launch_bounds__(kMxQuantThreads, 3) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint4* scales, uint32_t rows, uint32_t chunks,
                                                              uint32_t blocks, uint32_t C8) {
   __shared__ __align__(16) uint32_t image[128];
   grid_launch_dependents();

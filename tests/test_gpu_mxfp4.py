@@ -82,6 +82,14 @@ def test_extremes_and_non_numbers():
     _check_quantised(x)
 
 
+def test_no_rows():
+    codes, scales = api.ssconv_quantize_mxfp4(torch.empty(0, 40, dtype=torch.bfloat16, device=DEV))
+    assert codes.shape == (0, 32) and scales.numel() == 0
+    assert api.ssconv_dequantize_mxfp4(codes, scales, 40).shape == (0, 40)
+    with pytest.raises(api.SsconvError):
+        api.ssconv_quantize_mxfp4(torch.empty(4, 0, dtype=torch.bfloat16, device=DEV))
+
+
 def test_large_quantisation_in_pieces():
     rows, c = 70_001, 200
     x = _randn(9, rows, c).bfloat16()

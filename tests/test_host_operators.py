@@ -118,6 +118,10 @@ def test_residual_norm_refuses():
     assert _forward(_desc(pre=0), h=None, y=None) == NULL
     assert _forward(_desc(pre=0)) == BAD                         # y of no norm
     assert _forward(_desc(), h=32) == BAD                        # h and y in one buffer
+    n = 2 * 8 * 64                                               # bytes of a tensor
+    assert _forward(_desc(), x=4096, b=8192, h=4096 + 16, y=65536) == BAD
+    assert _forward(_desc(), x=4096, b=8192, h=65536, y=8192 - 16) == BAD
+    assert _forward(_desc(), x=4096, b=8192, h=65536, y=65536 + n - 16) == BAD
     assert _forward(_desc(), x=24) == ALIGN
     assert _forward(_desc(), gate=24) == ALIGN
     assert _forward(_desc(), params=(None, None, 24, None)) == ALIGN
@@ -139,9 +143,15 @@ def test_residual_norm_backward_refuses():
     assert _backward(_desc(), b=None) == NULL
     assert _backward(_desc(), sums=(None, 16, None, None, None)) == BAD   # a gradient of a norm that is not there
     assert _backward(_desc(pre=0, post=1), sums=(None, None, None, None, 16)) == BAD
+    far = dict(x=4096, b=8192, dh=16384, dy=32768, dx=65536, db=131072)
+    for name in ("dx", "db"):
+        for other in ("x", "b", "dh", "dy", "dx", "db"):
+            if other != name:
+                assert _backward(_desc(), **{**far, name: far[other]}) == BAD
+                assert _backward(_desc(), **{**far, name: far[other] + 16}) == BAD
     assert _backward(_desc(), dx=8) == ALIGN
-    assert _backward(_desc(), ws=None) == WORKSPACE
-    assert _backward(_desc(), ws_bytes=16) == WORKSPACE
+    assert _backward(_desc(), **far, ws=None) == WORKSPACE
+    assert _backward(_desc(), **far, ws_bytes=16) == WORKSPACE
 
 
 @pytest.mark.parametrize("rows,rows_per_gate,c", [(1, 0, 8), (7, 7, 96), (7, 100, 96), (1 << 20, 1, 8), (401408, 0, 96), (401408, 3136, 96),
