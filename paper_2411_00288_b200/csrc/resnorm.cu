@@ -66,22 +66,24 @@ __device__ __forceinline__ void params8(const float* p, int piece, bool live, fl
   const ulonglong2 a = reinterpret_cast<const ulonglong2*>(p)[2 * piece], b = reinterpret_cast<const ulonglong2*>(p)[2 * piece + 1];
   v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
 }
-// A vector of parameters as a thread uses it: with one piece per thread the piece stays in registers, else it is loaded (from L1)
-// for every row.
-template <bool HELD>
+// A vector of parameters as a thread uses it: its pieces stay in registers, or (not HELD) are loaded, from L1, for every row.
+template <int V, bool HELD>
 struct Params {
   const float* p = nullptr;
   float otherwise = 0.0f;
-  Pair held[4];
-  __device__ __forceinline__ void set(const float* from, float without, int piece, bool live) {
+  Pair held[HELD ? V : 1][4];
+  __device__ __forceinline__ void set(const float* from, float without, int sub, int run, const bool (&live)[V]) {
     p = from;
     otherwise = without;
-    if (HELD) params8(from, piece, live, without, held);
-  }
-  __device__ __forceinline__ void get(int piece, bool live, Pair (&v)[4]) const {
     if (HELD) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = held[j];
+      for (int k = 0; k < V; ++k) params8(from, sub + k * run, live[k], without, held[k]);
+    }
+  }
+  __device__ __forceinline__ void get(int k, int piece, bool live, Pair (&v)[4]) const {
+    if (HELD) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = held[k][j];
     } else {
       params8(p, piece, live, otherwise, v);
     }
@@ -272,13 +274,13 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
   grid_dependency_wait();
 #pragma unroll
   for (int d = 0; d < kForwardDepth - 1; ++d) fetch();
-  constexpr bool kHeld = V == 1;
-  Params<kHeld> gates, post_gamma, post_beta, pre_gamma, pre_beta;
-  gates.set(p.rows_per_gate == 0 ? p.t.gate : nullptr, 1.0f, sub, own[0]);
-  if (POST) post_gamma.set(p.t.post_gamma, 1.0f, sub, own[0]);
-  if (POST) post_beta.set(p.t.post_beta, 0.0f, sub, own[0]);
-  if (PRE) pre_gamma.set(p.t.pre_gamma, 1.0f, sub, own[0]);
-  if (PRE) pre_beta.set(p.t.pre_beta, 0.0f, sub, own[0]);
+  constexpr bool kHeld = V == 1 || !BLOCK;
+  Params<V, kHeld> gates, post_gamma, post_beta, pre_gamma, pre_beta;
+  gates.set(p.rows_per_gate == 0 ? p.t.gate : nullptr, 1.0f, sub, run, own);
+  if (POST) post_gamma.set(p.t.post_gamma, 1.0f, sub, run, own);
+  if (POST) post_beta.set(p.t.post_beta, 0.0f, sub, run, own);
+  if (PRE) pre_gamma.set(p.t.pre_gamma, 1.0f, sub, run, own);
+  if (PRE) pre_beta.set(p.t.pre_beta, 0.0f, sub, run, own);
   int gates_end = p.rows_per_gate > 0 ? 0 : p.rows;  // the first row with other gates
   const Pair scale = both(p.scale);
   for (; row - team < last; row += kTeams, here += stride) {
@@ -296,17 +298,17 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
     if (there && row >= gates_end) {
       const int image = row / p.rows_per_gate;
       gates_end = (int)min((int64_t)p.rows, (int64_t)(image + 1) * p.rows_per_gate);
-      gates.set(p.t.gate != nullptr ? p.t.gate + (int64_t)image * (8 * C8) : p.t.gate, 1.0f, sub, own[0]);
+      gates.set(p.t.gate != nullptr ? p.t.gate + (int64_t)image * (8 * C8) : p.t.gate, 1.0f, sub, run, own);
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const int piece = sub + k * run;
       Pair g[4];
-      gates.get(piece, own[k], g);
+      gates.get(k, piece, own[k], g);
       if (POST) {
         Pair a[4], c[4];
-        post_gamma.get(piece, own[k], a);
-        post_beta.get(piece, own[k], c);
+        post_gamma.get(k, piece, own[k], a);
+        post_beta.get(k, piece, own[k], c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) bv[k][j] = fma2(mul2(add2(bv[k][j], both(-stats.x)), both(stats.y)), a[j], c[j]);
       }
@@ -320,8 +322,8 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
       for (int k = 0; k < V; ++k) {
         const int piece = sub + k * run;
         Pair a[4], c[4];
-        pre_gamma.get(piece, own[k], a);
-        pre_beta.get(piece, own[k], c);
+        pre_gamma.get(k, piece, own[k], a);
+        pre_beta.get(k, piece, own[k], c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) hv[k][j] = fma2(mul2(add2(hv[k][j], both(-stats.z)), both(stats.w)), a[j], c[j]);
         if (there && own[k]) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.t.y) + here + k * 16 * run) = pack8(hv[k]);
@@ -427,13 +429,13 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
   Place at = start_of(p, blockIdx.x * kCrewsPerBlock + (BLOCK ? 0 : threadIdx.x >> 5)), coming = at;
 #pragma unroll
   for (int d = 0; d < kDepth - 1; ++d) fetch(coming);
-  constexpr bool kHeld = V == 1;
-  Params<kHeld> gates, post_gamma, post_beta, pre_gamma;
-  const auto set_gates = [&] { gates.set(p.t.gate != nullptr && p.image_gates ? p.t.gate + (int64_t)at.image * C : p.t.gate, 1.0f, sub, own[0]); };
+  constexpr bool kHeld = V == 1 || !BLOCK;
+  Params<V, kHeld> gates, post_gamma, post_beta, pre_gamma;
+  const auto set_gates = [&] { gates.set(p.t.gate != nullptr && p.image_gates ? p.t.gate + (int64_t)at.image * C : p.t.gate, 1.0f, sub, run, own); };
   if (at.unit < p.units) set_gates();
-  if (POST) post_gamma.set(p.t.post_gamma, 1.0f, sub, own[0]);
-  if (POST) post_beta.set(p.t.post_beta, 0.0f, sub, own[0]);
-  if (PRE) pre_gamma.set(p.t.pre_gamma, 1.0f, sub, own[0]);
+  if (POST) post_gamma.set(p.t.post_gamma, 1.0f, sub, run, own);
+  if (POST) post_beta.set(p.t.post_beta, 0.0f, sub, run, own);
+  if (PRE) pre_gamma.set(p.t.pre_gamma, 1.0f, sub, run, own);
   const Pair scale = both(p.scale);
   while (at.unit < p.units) {
     fetch(coming);
@@ -464,10 +466,10 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
         Pair gv[4], a[4], c[4], g[4];
         unpack8(ring.read(4 * k + 1), hat[k]);
         unpack8(ring.read(4 * k + 2), gv);
-        gates.get(piece, own[k], g);
+        gates.get(k, piece, own[k], g);
         if (POST) {
-          post_gamma.get(piece, own[k], a);
-          post_beta.get(piece, own[k], c);
+          post_gamma.get(k, piece, own[k], a);
+          post_beta.get(k, piece, own[k], c);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -477,7 +479,7 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
           acc[kPreGamma][k][j] = fma2(gv[j], hat[k][j], acc[kPreGamma][k][j]);
           acc[kPreBeta][k][j] = add2(acc[kPreBeta][k][j], gv[j]);
         }
-        pre_gamma.get(piece, own[k], a);
+        pre_gamma.get(k, piece, own[k], a);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const Pair q = mul2(gv[j], a[j]);
@@ -513,10 +515,10 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_backward_k
         for (int j = 0; j < 4; ++j) o[j] = mul2(scale, d[k][j]);
         *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.g.dx) + here + k * 16 * run) = pack8(o);
       }
-      gates.get(piece, own[k], g);
+      gates.get(k, piece, own[k], g);
       if (POST) {
-        post_gamma.get(piece, own[k], a);
-        post_beta.get(piece, own[k], c);
+        post_gamma.get(k, piece, own[k], a);
+        post_beta.get(k, piece, own[k], c);
       }
       if (mine)
 #pragma unroll
@@ -660,12 +662,23 @@ int power_of_two_from(int n) {
   while (p < n) p <<= 1;
   return p;
 }
-// One piece per thread: parameters and sums of its channels then stay in its registers, and what is done once per row is
-// spread over the most threads.  us, forward / with gradients: 401408 x 96 one piece on 12 of 16 lanes 61 / 146, three pieces on
-// 4 lanes 64 / 160; 12017 x 1000 with both norms one piece on 128 threads 25 / 67, two on 64 30 / 97, four on a warp 33 / 107.
-// Rows of more than 4096 channels take two pieces.
-Team team_for(int C8) {
-  if (C8 <= 32) return {false, 1, power_of_two_from(C8), kCrewThreads};
+// Rows of up to 768 channels are part of a warp, with up to `most` pieces per lane: as few lane-pieces as hold a row, and of equal
+// ones the fewer lanes, because what is done once per row costs every lane the same.  Parameters and sums of a lane's channels
+// stay in its registers.  Longer rows are a block's, one piece per thread (two beyond 4096 channels), and so are those of more than
+// 256 channels where there are few rows, for their latency (49 x 768: 2.1 us instead of 4.1).
+// us, forward: 401408 x 96 on 16 lanes of one piece 62, on 4 of three 57; 25088 x 384 on a block of 64 threads 23.9, on 16 lanes of
+// three 15.8.
+Team team_for(int C8, int most, int64_t rows) {
+  const bool few = rows <= 4 * (int64_t)device_sms();
+  if (C8 <= 32 * (few ? 1 : most)) {
+    Team best = {false, 1, 1 << 20, kCrewThreads};
+    for (int V = few ? 1 : most; V >= 1; --V) {
+      const int lanes = power_of_two_from((C8 + V - 1) / V);
+      // (several pieces only where a row's lanes still load 64 bytes side by side: 400000 x 16 on one lane of two 15.8, on two 8.9)
+      if (lanes <= 32 && (V == 1 || lanes >= 4) && lanes * V < best.lanes * best.V) best = {false, V, lanes, kCrewThreads};
+    }
+    return best;
+  }
   const int V = C8 <= 512 ? 1 : 2;
   const int threads = (((C8 + V - 1) / V) + 31) / 32 * 32;
   return {true, V, threads, threads};
@@ -699,28 +712,32 @@ int resident_blocks(const void* kernel, int threads, int smem) {
   return blocks;
 }
 
-static_assert(forward_smem(2, 512) <= kMostSlots && backward_smem(1, 512) <= kMostSlots && backward_smem(2, 512) <= kMostSlots, "");
+static_assert(forward_smem(2, 512) <= kMostSlots && forward_smem(3, 256) <= kMostSlots && backward_smem(1, 512) <= kMostSlots && backward_smem(2, 512) <= kMostSlots, "");
 
 // The kernel of a team.
-#define SSCONV_TEAM_KERNEL(kernel)                                                                        \
-  if (t.block) return t.V == 1 ? kernel<32, 1, true, POST, PRE> : kernel<32, 2, true, POST, PRE>;         \
-  switch (t.lanes) {                                                                                      \
-    case 1: return kernel<1, 1, false, POST, PRE>;                                                        \
-    case 2: return kernel<2, 1, false, POST, PRE>;                                                        \
-    case 4: return kernel<4, 1, false, POST, PRE>;                                                        \
-    case 8: return kernel<8, 1, false, POST, PRE>;                                                        \
-    case 16: return kernel<16, 1, false, POST, PRE>;                                                      \
-    default: return kernel<32, 1, false, POST, PRE>;                                                      \
+#define SSCONV_LANES_KERNEL(kernel, V)                        \
+  switch (t.lanes) {                                          \
+    case 1: return kernel<1, V, false, POST, PRE>;            \
+    case 2: return kernel<2, V, false, POST, PRE>;            \
+    case 4: return kernel<4, V, false, POST, PRE>;            \
+    case 8: return kernel<8, V, false, POST, PRE>;            \
+    case 16: return kernel<16, V, false, POST, PRE>;          \
+    default: return kernel<32, V, false, POST, PRE>;          \
   }
 template <bool POST, bool PRE>
 void (*forward_kernel(const Team& t))(ForwardParams) {
-  SSCONV_TEAM_KERNEL(resnorm_kernel)
+  if (t.block) return t.V == 1 ? resnorm_kernel<32, 1, true, POST, PRE> : resnorm_kernel<32, 2, true, POST, PRE>;
+  if (t.V == 1) SSCONV_LANES_KERNEL(resnorm_kernel, 1)
+  if (t.V == 2) SSCONV_LANES_KERNEL(resnorm_kernel, 2)
+  SSCONV_LANES_KERNEL(resnorm_kernel, 3)
 }
 template <bool POST, bool PRE>
 void (*backward_kernel(const Team& t))(BackwardParams) {
-  SSCONV_TEAM_KERNEL(resnorm_backward_kernel)
+  if (t.block) return t.V == 1 ? resnorm_backward_kernel<32, 1, true, POST, PRE> : resnorm_backward_kernel<32, 2, true, POST, PRE>;
+  if (t.V == 1) SSCONV_LANES_KERNEL(resnorm_backward_kernel, 1)
+  SSCONV_LANES_KERNEL(resnorm_backward_kernel, 2)
 }
-#undef SSCONV_TEAM_KERNEL
+#undef SSCONV_LANES_KERNEL
 
 // How the backward pass is cut: units, and blocks (the scratch is sized by them).
 struct Cut {
@@ -728,12 +745,15 @@ struct Cut {
   int units, unit_rows, units_per_gate, gate_rows, blocks, images;
   bool image_gates;
 };
-constexpr int kBackwardWarps = 16;       // per SM, of crews at work at once
+constexpr int kBackwardWarps = 16;       // per SM, of crews at work at once; half as many where a lane has two pieces' sums in registers
 constexpr int kRowsPerTeam = 4;          // of a unit, at least: its sums are written once
 
 Cut cut_backward(const ssconv_resnorm_t& d) {
   Cut c;
-  c.team = team_for(d.C / 8);
+  // Two pieces with two norms or more than 256 channels, us of the gradients alone, one piece / two (/ three): 120170 x 96 with two norms
+  // 52 / 38 (/ 58), 25088 x 384 with one 42 / 34 (/ 50); but 401408 x 96 with one 86 / 91.
+  const bool both_norms = d.post != SSCONV_NORM_NONE && d.pre != SSCONV_NORM_NONE;
+  c.team = team_for(d.C / 8, both_norms || d.C > 256 ? 2 : 1, d.rows);
   c.image_gates = d.rows_per_gate > 0;
   const int64_t rows = d.rows;
   c.gate_rows = (int)(c.image_gates && d.rows_per_gate < rows ? d.rows_per_gate : rows);
@@ -741,7 +761,8 @@ Cut cut_backward(const ssconv_resnorm_t& d) {
   const int crew_warps = c.team.block ? c.team.threads / 32 : 1;
   const int teams = c.team.block ? 1 : 32 / c.team.lanes;
   const int crews_per_block = c.team.block ? 1 : c.team.threads / 32;
-  const int64_t most = (int64_t)device_sms() * (kBackwardWarps / crew_warps > 0 ? kBackwardWarps / crew_warps : 1);
+  const int warps = c.team.V > 1 && !c.team.block ? kBackwardWarps / 2 : kBackwardWarps;
+  const int64_t most = (int64_t)device_sms() * (warps / crew_warps > 0 ? warps / crew_warps : 1);
   // Units per row of gates: as many as keep the crew with the most rows short, fewer where it makes no difference.
   const int64_t worth = (c.gate_rows + teams * kRowsPerTeam - 1) / (teams * kRowsPerTeam);
   const int64_t all = most / c.images < 1 ? 1 : most / c.images;
@@ -769,7 +790,7 @@ Cut cut_backward(const ssconv_resnorm_t& d) {
 
 cudaError_t launch_resnorm(const ssconv_resnorm_t& d, const ResnormTensors& t, cudaStream_t st) {
   const int C8 = d.C / 8;
-  const Team team = team_for(C8);
+  const Team team = team_for(C8, 3, d.rows);
   const bool post = d.post != SSCONV_NORM_NONE, pre = d.pre != SSCONV_NORM_NONE && t.y != nullptr;
   const auto kernel = post ? (pre ? forward_kernel<true, true>(team) : forward_kernel<true, false>(team))
                            : (pre ? forward_kernel<false, true>(team) : forward_kernel<false, false>(team));

@@ -142,6 +142,13 @@ def test_norms_of_every_kind_and_width(c, post, pre):
     _check(Case(37, c, post=post, pre=pre, seed=c))
 
 
+# (past four rows per SM the rows of up to 768 channels are dealt to warps with several pieces per lane)
+@pytest.mark.parametrize("post,pre", [(NONE, LAYER), (RMS, NONE), (LAYER, RMS), (LAYER, LAYER), (NONE, NONE)])
+@pytest.mark.parametrize("c", [8, 16, 40, 48, 64, 88, 96, 120, 128, 192, 256, 264, 320, 384, 512, 520, 680, 768, 776])
+def test_many_rows_of_every_width(c, post, pre):
+    _check(Case(733, c, rows_per_gate=50 if c % 16 else 0, post=post, pre=pre, seed=c))
+
+
 @pytest.mark.parametrize("c", [2048, 4096, 4104, 8192])
 @pytest.mark.parametrize("post,pre", [(LAYER, RMS), (NONE, LAYER), (RMS, NONE), (LAYER, LAYER)])
 def test_wide_rows(c, post, pre):
