@@ -16,8 +16,8 @@ namespace {
 // ---------------------------------------------------------------------------------------
 // Quantisation.  The scale's exponent comes from the exponent field E of the block's largest magnitude: floor(log2) = E - 127, so
 // the code (bias 127) is E - 2, at least 0; E = 255 (an infinity or a NaN) gives 255.  Elements are multiplied by the inverse
-// power of two (exact) and rounded once.  A thread block takes the 128 rows x 128 channels of a scale image, 16 lanes a row and
-// four lanes a block of 32, each thread four rows: four loads in flight, and the image is written whole.  2.53 bytes per element;
+// power of two (exact) and rounded once.  A thread block takes the 128 rows x 128 channels of a scale image, four lanes a block of
+// 32 and LANES a row (16; 8 or 4 where rows have no more: 402714 x 8 19 us otherwise), and the image is written whole.  2.53 bytes per element;
 // 401408 x 96 in 22.9 us (4.3 TB/s; a quarter of the lanes have no channels there, and conversions and shuffles take their share),
 // 25088 x 1536 in 20.
 // ---------------------------------------------------------------------------------------
@@ -48,27 +48,29 @@ __device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, uint32_t scale_x2) {
   return out;
 }
 
-constexpr int kMxQuantThreads = 512, kMxRowsPerThread = 4;  // 32 rows of threads
+constexpr int kMxQuantThreads = 512;
 
+template <int LANES>
 __global__ void __launch_bounds__(kMxQuantThreads, 3) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint4* scales, uint32_t rows, uint32_t chunks,
                                                              uint32_t blocks, uint32_t C8) {
   __shared__ __align__(16) uint32_t image[128];
   grid_launch_dependents();
   const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
-  const uint32_t lane = threadIdx.x & 15u, r0 = threadIdx.x >> 4;
+  constexpr uint32_t kRows = kMxQuantThreads / LANES, kTurns = 128 / kRows;  // rows at a time
+  const uint32_t lane = threadIdx.x & (LANES - 1), r0 = threadIdx.x / LANES;
   const uint32_t piece = chunk * 16u + lane;  // of 8 channels
   const uint32_t there = rows - tile * 128u;  // rows from the tile's first on
   grid_dependency_wait();
-  uint4 v[kMxRowsPerThread];
+  uint4 v[kTurns];
 #pragma unroll
-  for (int u = 0; u < kMxRowsPerThread; ++u) {
-    const uint32_t r = r0 + 32u * u;
+  for (int u = 0; u < (int)kTurns; ++u) {
+    const uint32_t r = r0 + kRows * u;
     v[u] = make_uint4(0u, 0u, 0u, 0u);
     if (r < there && piece < C8) v[u] = x[(uint64_t)(tile * 128u + r) * C8 + piece];
   }
 #pragma unroll
-  for (int u = 0; u < kMxRowsPerThread; ++u) {
-    const uint32_t r = r0 + 32u * u;
+  for (int u = 0; u < (int)kTurns; ++u) {
+    const uint32_t r = r0 + kRows * u;
     constexpr uint32_t kMagnitudes = 0x7FFF7FFFu;
     uint32_t m = max_bf16x2(max_bf16x2(v[u].x & kMagnitudes, v[u].y & kMagnitudes), max_bf16x2(v[u].z & kMagnitudes, v[u].w & kMagnitudes));
     m = max_bf16x2(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
@@ -78,8 +80,8 @@ __global__ void __launch_bounds__(kMxQuantThreads, 3) quantize_mxfp4_kernel(cons
     const uint32_t inverse = ((254u - min(code, 252u)) << 7) * 0x10001u;
     if (r < there && (piece >> 2) < blocks) codes[(uint64_t)(tile * 128u + r) * (4u * blocks) + piece] = e2m1_x8(v[u], inverse);
     uint32_t word = code << (8u * (lane >> 2));
-    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
-    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
+    if (LANES > 4) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
+    if (LANES > 8) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
     if (lane == 0) image[(r & 31u) * 4u + (r >> 5)] = word;
   }
   __syncthreads();
@@ -94,19 +96,21 @@ __device__ __forceinline__ void e2m1_values_x4(uint32_t codes, uint32_t& low, ui
   low = __byte_perm(lo, hi, 0x5140) | ((codes << 12) & 0x8000u) | ((codes << 24) & 0x80000000u);
   high = __byte_perm(lo, hi, 0x7362) | ((codes << 4) & 0x8000u) | ((codes << 16) & 0x80000000u);
 }
+template <int LANES>
 __global__ void __launch_bounds__(kMxQuantThreads) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint32_t rows, uint32_t chunks,
                                                                uint32_t blocks, uint32_t C8) {
   grid_launch_dependents();
   const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
-  const uint32_t lane = threadIdx.x & 15u, r0 = threadIdx.x >> 4;
+  constexpr uint32_t kRows = kMxQuantThreads / LANES, kTurns = 128 / kRows;
+  const uint32_t lane = threadIdx.x & (LANES - 1), r0 = threadIdx.x / LANES;
   const uint32_t piece = chunk * 16u + lane;
   const uint32_t there = rows - tile * 128u;
   grid_dependency_wait();
   if (piece >= C8) return;
-  uint32_t c[kMxRowsPerThread], s[kMxRowsPerThread];
+  uint32_t c[kTurns], s[kTurns];
 #pragma unroll
-  for (int u = 0; u < kMxRowsPerThread; ++u) {
-    const uint32_t r = r0 + 32u * u;
+  for (int u = 0; u < (int)kTurns; ++u) {
+    const uint32_t r = r0 + kRows * u;
     c[u] = s[u] = 0u;
     if (r < there) {
       c[u] = codes[(uint64_t)(tile * 128u + r) * (4u * blocks) + piece];
@@ -114,8 +118,8 @@ __global__ void __launch_bounds__(kMxQuantThreads) dequantize_mxfp4_kernel(const
     }
   }
 #pragma unroll
-  for (int u = 0; u < kMxRowsPerThread; ++u) {
-    const uint32_t r = r0 + 32u * u;
+  for (int u = 0; u < (int)kTurns; ++u) {
+    const uint32_t r = r0 + kRows * u;
     // the scale as bf16: 2^-127 is below the normal numbers, 255 is a NaN
     const uint32_t scale = (s[u] == 255u ? 0x7FC0u : s[u] == 0u ? 0x0040u : s[u] << 7) * 0x10001u;
     uint4 o;
@@ -625,14 +629,16 @@ int32_t mx_device(int dev, int* pairs) {
 cudaError_t launch_quantize_mxfp4(const void* x, int64_t rows, int C, void* codes, void* scales, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
   count_launch();
-  return launch_dependent(quantize_mxfp4_kernel, (unsigned)(g.row_tiles * g.chunks), kMxQuantThreads, st, (const uint4*)x, (uint32_t*)codes, (uint4*)scales,
+  const auto kernel = g.blocks <= 1 ? quantize_mxfp4_kernel<4> : g.blocks <= 2 ? quantize_mxfp4_kernel<8> : quantize_mxfp4_kernel<16>;
+  return launch_dependent(kernel, (unsigned)(g.row_tiles * g.chunks), kMxQuantThreads, st, (const uint4*)x, (uint32_t*)codes, (uint4*)scales,
                           (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
 cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int C, void* x, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
   count_launch();
-  return launch_dependent(dequantize_mxfp4_kernel, (unsigned)(g.row_tiles * g.chunks), kMxQuantThreads, st, (const uint32_t*)codes, (const uint8_t*)scales,
+  const auto kernel = g.blocks <= 1 ? dequantize_mxfp4_kernel<4> : g.blocks <= 2 ? dequantize_mxfp4_kernel<8> : dequantize_mxfp4_kernel<16>;
+  return launch_dependent(kernel, (unsigned)(g.row_tiles * g.chunks), kMxQuantThreads, st, (const uint32_t*)codes, (const uint8_t*)scales,
                           (uint4*)x, (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
