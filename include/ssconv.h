@@ -491,7 +491,7 @@ int32_t ssconv_forward_dense_fp8(const ssconv_desc_t* desc, const void* x_e4m3, 
  * all layers' tensors at once.  Tensors are given by HOST arrays of device pointers and element counts, read before the call
  * returns; `type` (nullable: all SSCONV_F32) holds SSCONV_F32 or SSCONV_BF16 per tensor.  Pointers need the alignment of their
  * elements (16-byte ones are read faster); n[i] = 0 is allowed, its pointer is then ignored.  SSCONV_ERR_BAD_DESC: a negative
- * count, an unknown type, written tensors that overlap other tensors of the call (the same one twice, say; out[i] == g[i] is
+ * count, an unknown type, written memory that overlaps other memory of the call (the same tensor twice, say; out[i] == g[i] is
  * allowed). SSCONV_ERR_UNSUPPORTED_SHAPE: more than 2^40 elements.  No counterpart in the paper: it updates one layer's weights
  * at a time and does not clip.
  *
@@ -501,7 +501,8 @@ int32_t ssconv_forward_dense_fp8(const ssconv_desc_t* desc, const void* x_e4m3, 
  *   infinite).  norm: device fp32 [1]; ws: device scratch of ssconv_grad_norm_ws_bytes(tensors) bytes, 8-byte aligned, that no
  *   other call in flight uses.
  * ssconv_clip_grads:  out[i] = g[i] * min(1, max_norm / (norm + 1e-6)), in the type of g[i], rounded once; norm as written by
- *   ssconv_grad_norm.  A NaN norm makes all gradients NaN, an infinite one makes the finite ones 0.
+ *   ssconv_grad_norm.  A NaN norm makes all gradients NaN, an infinite one makes the finite ones 0 (NaN
+ *   if max_norm is infinite too).
  * ssconv_adamw_multi:  ssconv_adamw's update of every tensor with g[i] scaled as by ssconv_clip_grads (norm = NULL: not scaled);
  *   theta, m, v: fp32; `type` is that of g.  The hyperparameters are doubles: 1 - beta is taken before rounding to fp32. */
 enum { SSCONV_F32 = 0, SSCONV_BF16 = 1 };
@@ -524,8 +525,8 @@ int32_t ssconv_adamw_multi(void* const* theta, const void* const* g, void* const
  * or SSCONV_NORM_RMS (v / sqrt(mean(v^2) + eps) * gamma + beta).  gamma, beta: fp32 [C], NULL for ones and zeros.  gate: fp32,
  * NULL (ones), [C] with rows_per_gate = 0, or [ceil(rows / rows_per_gate)][C]: row r takes gates r / rows_per_gate.  x, b, h, y: bf16
  * [rows][C]; arithmetic in fp32, y is the norm of h before h is rounded.  stats (nullable): fp32 [rows][4], what the backward call
- * needs of both norms (mean and 1/deviation of b, then of h).  h (nullable if y is wanted) and y may be the buffer of x or of b
- * (overlapping them in another way, or each other, is SSCONV_ERR_BAD_DESC).
+ * needs of both norms (mean and 1/deviation of b, then of h).  h (nullable if y is wanted) and y may be the buffer of x or of b;
+ * any other overlap of what is written is SSCONV_ERR_BAD_DESC.
  * C % 8 == 0, C <= 8192, rows <= 2^30 (rows = 0 is a no-op); tensors 16-byte aligned. */
 enum { SSCONV_NORM_NONE = 0, SSCONV_NORM_LAYER = 1, SSCONV_NORM_RMS = 2 };
 typedef struct {
@@ -540,8 +541,8 @@ int32_t ssconv_residual_norm(const ssconv_resnorm_t* desc, const void* x, const 
  * [rows][C]; dgate of the shape of gate; dpost_gamma, dpost_beta, dpre_gamma, dpre_beta fp32 [C]: sums over rows in fp32, in a fixed
  * order.  Any output may be NULL (not computed); those of a norm that is not there must be.  stats: as the forward call wrote them
  * (ignored without norms).  rows = 0 writes zeros to dgate (if shared) and to the gradients of the norms' parameters.  ws: device
- * scratch of ssconv_residual_norm_ws_bytes bytes, 16-byte aligned, that no other call in flight uses.  dx and db must not overlap
- * inputs or each other (SSCONV_ERR_BAD_DESC). */
+ * scratch of ssconv_residual_norm_ws_bytes bytes, 16-byte aligned, that no other call in flight uses.  What is written must not
+ * overlap inputs or each other (SSCONV_ERR_BAD_DESC). */
 int32_t ssconv_residual_norm_ws_bytes(const ssconv_resnorm_t* desc, size_t* bytes);
 int32_t ssconv_residual_norm_backward(const ssconv_resnorm_t* desc, const void* x, const void* b, const float* stats,
                                       const void* dh, const void* dy, const float* gate, const float* post_gamma,
@@ -558,7 +559,8 @@ int32_t ssconv_residual_norm_backward(const ssconv_resnorm_t* desc, const void* 
  * go in with their zeros).
  *   codes:  [rows][ceil(C/32) * 16] bytes, two channels per byte, the lower one in the low half, zeros past C.
  *   scales: bytes in the tile order of the tensor-core instruction, padded to whole tiles; every byte of both is written.
- * ssconv_sizes_mxfp4 gives the sizes of both.  x: bf16 [rows][C], 16-byte aligned; C % 8 == 0; rows >= 0. */
+ * ssconv_sizes_mxfp4 gives the sizes of both.  x: bf16 [rows][C], 16-byte aligned; C % 8 == 0; rows >= 0.
+ * As in the calls below, what is written must not overlap anything else of the call (SSCONV_ERR_BAD_DESC). */
 int32_t ssconv_sizes_mxfp4(int64_t rows, int32_t C, size_t* code_bytes, size_t* scale_bytes);
 int32_t ssconv_quantize_mxfp4(const void* x_bf16, int64_t rows, int32_t C, void* codes, void* scales, void* stream);
 /* The values the codes stand for (exact in bf16). */

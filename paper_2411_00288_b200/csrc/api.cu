@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <iterator>
 #include <new>
 #include <vector>
 
@@ -182,23 +183,23 @@ void add_spans(std::vector<Span>& spans, const void* const* p, const int64_t* n,
     spans.push_back({a, a + (uintptr_t)n[i] * (type != nullptr && type[i] == SSCONV_BF16 ? 2 : 4), written});
   }
 }
-bool written_once(std::vector<Span>& spans) {
-  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.begin < b.begin; });
+Span span_of(const void* p, size_t bytes, bool written) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  return {a, p ? a + bytes : a, written};  // (a null pointer: nothing)
+}
+bool written_once(Span* spans, Span* end) {
+  std::sort(spans, end, [](const Span& a, const Span& b) { return a.begin < b.begin; });
   uintptr_t read = 0, written = 0;  // furthest ends so far
-  for (const Span& s : spans) {
+  for (; spans != end; ++spans) {
+    const Span& s = *spans;
+    if (s.begin == s.end) continue;
     if (s.begin < written || (s.written && s.begin < read)) return false;
     uintptr_t& last = s.written ? written : read;
     last = std::max(last, s.end);
   }
   return true;
 }
-
-// Whether two buffers of that many bytes share memory without being the same one.
-bool overlap_partly(const void* a, const void* b, size_t bytes) {
-  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-  return a && b && p != q && p < q + bytes && q < p + bytes;
-}
-bool overlap(const void* a, const void* b, size_t bytes) { return a && (a == b || overlap_partly(a, b, bytes)); }
+bool written_once(std::vector<Span>& spans) { return written_once(spans.data(), spans.data() + spans.size()); }
 
 int32_t check_resnorm(const ssconv_resnorm_t* d) {
   if (!d) return SSCONV_ERR_NULL;
@@ -210,6 +211,11 @@ int32_t check_resnorm(const ssconv_resnorm_t* d) {
   return SSCONV_OK;
 }
 
+// Rows of gates.
+size_t resnorm_gates(const ssconv_resnorm_t& d) {
+  return d.rows_per_gate == 0 || d.rows_per_gate >= d.rows ? 1 : (size_t)((d.rows + d.rows_per_gate - 1) / d.rows_per_gate);
+}
+
 int32_t check_mxfp4(int64_t rows, int32_t C) {
   if (rows < 0 || C <= 0) return SSCONV_ERR_BAD_DESC;
   if (C % 8 != 0 || rows > 0x7FFFFF00LL) return SSCONV_ERR_UNSUPPORTED_SHAPE;
@@ -217,6 +223,14 @@ int32_t check_mxfp4(int64_t rows, int32_t C) {
   // (row, chunk of 128 channels) pairs and pieces of 8 channels are numbered in 32 bits, blocks of 256 pieces in 31
   if (g.row_tiles * 128 * g.chunks > 0xFFFFFF00LL) return SSCONV_ERR_UNSUPPORTED_SHAPE;
   return SSCONV_OK;
+}
+size_t code_bytes_of(const ssconv::MxGeometry& g, int64_t rows) { return (size_t)rows * g.blocks * 16; }
+size_t scale_bytes_of(const ssconv::MxGeometry& g) { return (size_t)g.row_tiles * g.chunks * ssconv::kMxImageBytes; }
+bool apart_mxfp4(const void* x, int64_t rows, int32_t C, const void* codes, const void* scales, bool to_codes) {
+  const ssconv::MxGeometry g = ssconv::mx_geometry(rows, C);
+  Span spans[] = {span_of(x, 2 * (size_t)rows * C, !to_codes), span_of(codes, code_bytes_of(g, rows), to_codes),
+                  span_of(scales, scale_bytes_of(g), to_codes)};
+  return written_once(std::begin(spans), std::end(spans));
 }
 
 }  // namespace
@@ -1107,7 +1121,15 @@ int32_t ssconv_grad_norm(const void* const* g, const int64_t* n, const int32_t* 
   rc = check_list(g, n, type, tensors);
   if (rc != SSCONV_OK) return rc;
   if ((reinterpret_cast<uintptr_t>(norm) & 3u) || (reinterpret_cast<uintptr_t>(ws) & 7u)) return SSCONV_ERR_ALIGNMENT;
-  if (!ws || ws_bytes < ssconv::grad_norm_scratch(tensors)) return SSCONV_ERR_WORKSPACE;
+  const size_t scratch = ssconv::grad_norm_scratch(tensors);
+  if (!ws || ws_bytes < scratch) return SSCONV_ERR_WORKSPACE;
+  const Span written[2] = {span_of(norm, sizeof(float), true), span_of(ws, scratch, true)};
+  const auto apart = [](const Span& a, const Span& b) { return a.end <= b.begin || b.end <= a.begin; };
+  if (!apart(written[0], written[1])) return SSCONV_ERR_BAD_DESC;
+  for (int32_t i = 0; i < tensors; ++i) {
+    const Span read = span_of(g[i], (size_t)n[i] * (type != nullptr && type[i] == SSCONV_BF16 ? 2 : 4), false);
+    if (n[i] != 0 && !(apart(read, written[0]) && apart(read, written[1]))) return SSCONV_ERR_BAD_DESC;
+  }
   return ssconv::launch_grad_norm(g, n, type, tensors, kind == SSCONV_GRAD_NORM_INF, norm, static_cast<double*>(ws), (cudaStream_t)stream) ==
                  cudaSuccess
              ? SSCONV_OK
@@ -1128,7 +1150,8 @@ int32_t ssconv_clip_grads(const void* const* g, void* const* out, const int64_t*
   }
   try {
     std::vector<Span> spans;
-    spans.reserve(2 * (size_t)tensors);
+    spans.reserve(2 * (size_t)tensors + 1);
+    spans.push_back(span_of(norm, sizeof(float), false));
     add_spans(spans, out, n, type, tensors, true);
     add_spans(spans, g, n, type, tensors, false, out);
     if (!written_once(spans)) return SSCONV_ERR_BAD_DESC;
@@ -1156,7 +1179,8 @@ int32_t ssconv_adamw_multi(void* const* theta, const void* const* g, void* const
   }
   try {
     std::vector<Span> spans;
-    spans.reserve(4 * (size_t)tensors);
+    spans.reserve(4 * (size_t)tensors + 1);
+    spans.push_back(span_of(norm, sizeof(float), false));
     for (void* const* list : {theta, m, v}) add_spans(spans, const_cast<const void* const*>(list), n, nullptr, tensors, true);
     add_spans(spans, g, n, type, tensors, false);
     if (!written_once(spans)) return SSCONV_ERR_BAD_DESC;
@@ -1181,10 +1205,14 @@ int32_t ssconv_residual_norm(const ssconv_resnorm_t* desc, const void* x, const 
   for (const void* p : {x, b, (const void*)gate, (const void*)post_gamma, (const void*)post_beta, (const void*)pre_gamma, (const void*)pre_beta,
                         (const void*)h, (const void*)y, (const void*)stats})
     if (!aligned16(p)) return SSCONV_ERR_ALIGNMENT;
-  const size_t bytes = 2 * (size_t)desc->rows * desc->C;
-  if (overlap(h, y, bytes)) return SSCONV_ERR_BAD_DESC;
-  for (const void* in : {x, b})
-    if (overlap_partly(h, in, bytes) || overlap_partly(y, in, bytes)) return SSCONV_ERR_BAD_DESC;
+  const size_t bytes = 2 * (size_t)desc->rows * desc->C, row = 4 * (size_t)desc->C;
+  // (a row of x and b is read by the threads that then write h's and y's)
+  const auto input = [&](const void* in) { return span_of(in == h || in == y ? nullptr : in, bytes, false); };
+  Span spans[] = {span_of(h, bytes, true),        span_of(y, bytes, true),       span_of(stats, 16 * (size_t)desc->rows, true),
+                  input(x),                       input(b),                      span_of(gate, row * resnorm_gates(*desc), false),
+                  span_of(post_gamma, row, false), span_of(post_beta, row, false), span_of(pre_gamma, row, false),
+                  span_of(pre_beta, row, false)};
+  if (!written_once(std::begin(spans), std::end(spans))) return SSCONV_ERR_BAD_DESC;
   return ssconv::launch_resnorm(*desc, {x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, h, y, stats}, (cudaStream_t)stream) == cudaSuccess
              ? SSCONV_OK
              : SSCONV_ERR_CUDA;
@@ -1216,11 +1244,16 @@ int32_t ssconv_residual_norm_backward(const ssconv_resnorm_t* desc, const void* 
     return SSCONV_OK;
   }
   if (!x || !b || ((post || pre) && !stats) || (pre && !dy) || (!pre && !dh)) return SSCONV_ERR_NULL;
-  const size_t bytes = 2 * (size_t)desc->rows * desc->C;
-  if (overlap(dx, db, bytes)) return SSCONV_ERR_BAD_DESC;
-  for (const void* in : {x, b, dh, dy})
-    if (overlap(dx, in, bytes) || overlap(db, in, bytes)) return SSCONV_ERR_BAD_DESC;
-  if (!ws || ws_bytes < ssconv::resnorm_scratch(*desc)) return SSCONV_ERR_WORKSPACE;
+  const size_t scratch = ssconv::resnorm_scratch(*desc);
+  if (!ws || ws_bytes < scratch) return SSCONV_ERR_WORKSPACE;
+  const size_t bytes = 2 * (size_t)desc->rows * desc->C, row = 4 * (size_t)desc->C, gates = row * resnorm_gates(*desc);
+  Span spans[] = {span_of(dx, bytes, true),          span_of(db, bytes, true),         span_of(dgate, gates, true),
+                  span_of(dpost_gamma, row, true),   span_of(dpost_beta, row, true),   span_of(dpre_gamma, row, true),
+                  span_of(dpre_beta, row, true),     span_of(ws, scratch, true),       span_of(x, bytes, false),
+                  span_of(b, bytes, false),          span_of(dh, bytes, false),        span_of(pre ? dy : nullptr, bytes, false),
+                  span_of(post || pre ? stats : nullptr, 16 * (size_t)desc->rows, false), span_of(gate, gates, false),
+                  span_of(post_gamma, row, false),   span_of(post_beta, row, false),   span_of(pre_gamma, row, false)};
+  if (!written_once(std::begin(spans), std::end(spans))) return SSCONV_ERR_BAD_DESC;
   return ssconv::launch_resnorm_backward(*desc, {x, b, gate, post_gamma, post_beta, pre_gamma, nullptr, nullptr, nullptr, const_cast<float*>(stats)},
                                          {dh, dy, dx, db, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta}, static_cast<float*>(ws),
                                          (cudaStream_t)stream) == cudaSuccess
@@ -1232,8 +1265,8 @@ int32_t ssconv_sizes_mxfp4(int64_t rows, int32_t C, size_t* code_bytes, size_t* 
   const int32_t rc = check_mxfp4(rows, C);
   if (rc != SSCONV_OK) return rc;
   const ssconv::MxGeometry g = ssconv::mx_geometry(rows, C);
-  if (code_bytes) *code_bytes = (size_t)rows * g.blocks * 16;
-  if (scale_bytes) *scale_bytes = (size_t)g.row_tiles * g.chunks * ssconv::kMxImageBytes;
+  if (code_bytes) *code_bytes = code_bytes_of(g, rows);
+  if (scale_bytes) *scale_bytes = scale_bytes_of(g);
   return SSCONV_OK;
 }
 
@@ -1243,6 +1276,7 @@ int32_t ssconv_quantize_mxfp4(const void* x_bf16, int64_t rows, int32_t C, void*
   if (rows == 0) return SSCONV_OK;
   if (!x_bf16 || !codes || !scales) return SSCONV_ERR_NULL;
   if (!aligned16(x_bf16) || !aligned16(codes) || !aligned16(scales)) return SSCONV_ERR_ALIGNMENT;
+  if (!apart_mxfp4(x_bf16, rows, C, codes, scales, true)) return SSCONV_ERR_BAD_DESC;
   return ssconv::launch_quantize_mxfp4(x_bf16, rows, C, codes, scales, (cudaStream_t)stream) == cudaSuccess ? SSCONV_OK : SSCONV_ERR_CUDA;
 }
 
@@ -1252,6 +1286,7 @@ int32_t ssconv_dequantize_mxfp4(const void* codes, const void* scales, int64_t r
   if (rows == 0) return SSCONV_OK;
   if (!x_bf16 || !codes || !scales) return SSCONV_ERR_NULL;
   if (!aligned16(x_bf16) || !aligned16(codes) || !aligned16(scales)) return SSCONV_ERR_ALIGNMENT;
+  if (!apart_mxfp4(x_bf16, rows, C, codes, scales, false)) return SSCONV_ERR_BAD_DESC;
   return ssconv::launch_dequantize_mxfp4(codes, scales, rows, C, x_bf16, (cudaStream_t)stream) == cudaSuccess ? SSCONV_OK : SSCONV_ERR_CUDA;
 }
 
@@ -1267,6 +1302,13 @@ int32_t ssconv_forward_dense_mxfp4(const ssconv_desc_t* desc, const void* x_code
   if ((desc->flags & SSCONV_FLAG_BIAS) && !bias) return SSCONV_ERR_NULL;
   for (const void* p : {x_codes, x_scales, w_codes, w_scales, (const void*)bias, (const void*)y})
     if (!aligned16(p)) return SSCONV_ERR_ALIGNMENT;
+  const int64_t rows = (int64_t)desc->N * desc->H * desc->W;
+  const ssconv::MxGeometry gx = ssconv::mx_geometry(rows, desc->C_in), gw = ssconv::mx_geometry(desc->C_out, desc->C_in);
+  Span spans[] = {span_of(y, 2 * (size_t)rows * desc->C_out, true),      span_of(dev_status, sizeof(int32_t), true),
+                  span_of(x_codes, code_bytes_of(gx, rows), false),      span_of(x_scales, scale_bytes_of(gx), false),
+                  span_of(w_codes, code_bytes_of(gw, desc->C_out), false), span_of(w_scales, scale_bytes_of(gw), false),
+                  span_of(desc->flags & SSCONV_FLAG_BIAS ? bias : nullptr, 4 * (size_t)desc->C_out, false)};
+  if (!written_once(std::begin(spans), std::end(spans))) return SSCONV_ERR_BAD_DESC;
   return ssconv::launch_forward_mxfp4(*desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status, (cudaStream_t)stream);
 }
 

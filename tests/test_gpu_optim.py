@@ -249,3 +249,16 @@ def test_refusals():
         api.ssconv_adamw_multi(g, g, g, g, 0)
     with pytest.raises(api.SsconvError):
         api.ssconv_grad_norm(g, ws=torch.empty(8, dtype=torch.uint8, device=DEV))
+
+
+def test_bounds_at_the_ends():
+    """max_norm = 0 leaves zeros, an infinite one leaves the gradients (NaN if the norm is infinite too)."""
+    g = torch.randn(1000, device="cuda")
+    norm = api.ssconv_grad_norm([g])
+    out = [torch.empty_like(g)]
+    api.ssconv_clip_grads([g], norm, 0.0, out=out)
+    assert torch.equal(out[0], g * 0)
+    api.ssconv_clip_grads([g], norm, math.inf, out=out)
+    assert torch.equal(out[0], g)
+    api.ssconv_clip_grads([g], torch.full_like(norm, math.inf), math.inf, out=out)
+    assert out[0].isnan().all()

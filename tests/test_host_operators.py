@@ -222,3 +222,59 @@ def test_python_calls_refuse_what_is_not_on_the_gpu():
         api.ssconv_adamw_multi([1], [2], [3], [4], 1)
     with pytest.raises(ValueError):
         api.ssconv_dequantize_mxfp4(x.view(torch.uint8), f.view(torch.uint8), 40)
+
+
+def test_refuses_overlaps_of_what_is_written():
+    """Every written buffer against every other one of its call; launches nothing, so any addresses will do."""
+    f = api.lib()
+    K = 1 << 20
+    assert _norm([K], _counts(4), norm=K + 12, ws=64 * K) == BAD        # the norm inside a gradient
+    assert _norm([K], _counts(4), norm=2 * K, ws=K - 8) == BAD          # the scratch reaches into one
+    assert _norm([K], _counts(4), norm=64 * K + 4, ws=64 * K) == BAD    # the norm inside the scratch
+    g, out = _arrays([K], [2 * K])
+    assert f.ssconv_clip_grads(g, out, _counts(4), None, 1, 2 * K + 4, 1.0, None) == BAD
+    theta, g, m, v = _arrays([K], [2 * K], [3 * K], [4 * K])
+    assert f.ssconv_adamw_multi(theta, g, m, v, _counts(4), None, 1, 1, 1.0, 0.9, 0.999, 1e-8, 0.0, 3 * K + 4, 1.0, None) == BAD
+
+    d = ctypes.byref(api.make_resnorm(64, 64, rows_per_gate=16, post=api.NORM_LAYER, pre=api.NORM_RMS))
+    forward = [(i + 1) * K for i in range(10)]                           # x, b, gate, gammas and betas, h, y, stats
+    backward = [(i + 1) * K for i in range(16)]                          # x, b, stats, dh, dy, gate, gammas, outputs, ws
+    last = {"gate": 4 * 64 * 4 - 16, "row": 4 * 64 - 16, "stats": 64 * 16 - 16, "rows": 2 * 64 * 64 - 16}
+    inputs = ["rows", "rows", "gate", "row", "row", "row", "row"]
+    for written in (7, 8, 9):
+        for other in range(10):
+            if other == written:
+                continue
+            a = list(forward)
+            size = (inputs + ["rows", "rows", "stats"])[other]
+            a[written] = a[other] + last[size]                           # its first 16 bytes are the other's last ones
+            assert f.ssconv_residual_norm(d, *a, None) == BAD, (written, other)
+    kinds = ["rows", "rows", "stats", "rows", "rows", "gate", "row", None, "row", "rows", "rows", "gate", "row", "row", "row", "row"]
+    for written in range(9, 16):
+        for other in range(16):
+            if other == written or kinds[other] is None:                 # (post_beta has no part in the gradients)
+                continue
+            a = list(backward)
+            a[written] = a[other] + last[kinds[other]]
+            assert f.ssconv_residual_norm_backward(d, *a, 64 * K, 1 << 30, None) == BAD, (written, other)
+    for other in range(7):
+        a = list(backward)
+        a[other] = 64 * K + 16                                           # inside the scratch
+        assert f.ssconv_residual_norm_backward(d, *a, 64 * K, 1 << 30, None) == BAD, other
+
+    for call in (lambda a: f.ssconv_quantize_mxfp4(a[0], 4, 64, a[1], a[2], None), lambda a: f.ssconv_dequantize_mxfp4(a[1], a[2], 4, 64, a[0], None)):
+        ends = (4 * 64 * 2 - 16, 4 * 32 - 16)
+        assert call([K, K + ends[0], 3 * K]) == BAD
+        assert call([K, 2 * K, K + ends[0]]) == BAD
+    assert f.ssconv_quantize_mxfp4(K, 4, 64, 2 * K, 2 * K + 4 * 32 - 16, None) == BAD
+    desc = ctypes.byref(api.make_desc(1, 2, 2, 64, 64, 1, 1, bias=True))
+    base = [K, 2 * K, 3 * K, 4 * K, 5 * K, 6 * K, 7 * K]                 # codes and scales of x and w, bias, y, dev_status
+    ends = [4 * 32, 512, 64 * 32, 512, 64 * 4, 4 * 64 * 2]
+    for other in range(5):
+        a = list(base)
+        a[5] = a[other] + ends[other] - 16
+        assert f.ssconv_forward_dense_mxfp4(desc, *a, None) == BAD, other
+    for other in range(6):
+        a = list(base)
+        a[6] = a[other] + ends[other] - 4
+        assert f.ssconv_forward_dense_mxfp4(desc, *a, None) == BAD, other
