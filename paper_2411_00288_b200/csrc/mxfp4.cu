@@ -468,8 +468,6 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
         // a row's 64 outputs per lane; the next 16 columns are on their way
         uint32_t r[2][16];
         tc_ld_32x32b_x16(acc + 64 * g, r[0]);
-        if (lane == 0) bulk_wait_group_read0();  // the warp's last piece has left its buffer
-        __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           ulonglong2 bias[4];
@@ -492,6 +490,10 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
                 : "l"(f32x2(__uint_as_float(r[i & 1][2 * j]), __uint_as_float(r[i & 1][2 * j + 1]))), "l"(j & 1 ? bias[j >> 1].y : bias[j >> 1].x));
             split2(v, lo, hi);
             w[j] = activate_pack<ACT>(lo, hi);
+          }
+          if (i == 0) {  // (not before: 401408 x 96 -> 384 93.8 us instead of 97.3, 12544 x 2048 -> 512 11.7 instead of 12.3)
+            if (lane == 0) bulk_wait_group_read0();  // the warp's last piece has left its buffer
+            __syncwarp();
           }
           *reinterpret_cast<uint4*>(out + lane * 128 + (((2 * i) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
           *reinterpret_cast<uint4*>(out + lane * 128 + (((2 * i + 1) ^ (lane & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
