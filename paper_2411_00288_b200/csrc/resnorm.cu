@@ -609,47 +609,64 @@ struct FinishParams {
   int kind[kSums];            // ... and where they are among a block's
   int wanted, blocks, C;
   int images, units_per_gate; // of gates per image whose units were several (0 images: none)
+  int block_shift, image_shift;  // base-2 logarithms of R
   float* dgate;
 };
-// First the sums over blocks, 32 columns x 32 rows of threads; then those of the images' units, 4 columns per thread.
+// 4 columns per thread and 1024 / R threads side by side; the R threads of the same columns share the rows, so that none adds up
+// hundreds of them by itself.  (R = 1 for the images, us of the gradients: 4 images of 100352 x 96 121, 99 so; R = 32: 61 images of
+// 197 x 1000 71, 47 so.)  First the sums over blocks, then those of the images' units.
 __global__ void __launch_bounds__(1024) resnorm_finish_kernel(const FinishParams p) {
-  __shared__ float part[32][33];
+  __shared__ float4 part[1024];
   grid_launch_dependents();
   grid_dependency_wait();
-  const int groups = (p.C + 31) / 32;
-  int job = blockIdx.x;
-  if (job < groups * p.wanted) {
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const int which = job / groups, col = (job - which * groups) * 32 + tx;
-    const float* in = p.block_sums + (int64_t)p.kind[which] * p.C + col;
-    const int64_t pitch = (int64_t)kSums * p.C;
-    float s = 0.0f;
-    if (col < p.C) {
-#pragma unroll 8
-      for (int r = ty; r < p.blocks; r += 32) s += in[r * pitch];
-    }
-    part[ty][tx] = s;
-    __syncthreads();
-    s = part[tx][ty];  // column ty of the group, row tx of the partial sums
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xFFFFFFFFu, s, o);
-    const int c = col - tx + ty;
-    if (tx == 0 && c < p.C) p.out[which][c] = s;
-    return;
+  const int C4 = p.C / 4, groups = (C4 + (1024 >> p.block_shift) - 1) >> (10 - p.block_shift), job = blockIdx.x - groups * p.wanted;
+  const bool images = job >= 0;
+  const int shift = images ? p.image_shift : p.block_shift;  // R = 1 << shift
+  const int side = 1024 >> shift, r = threadIdx.x >> (10 - shift);
+  const float4* in;
+  float4* out;
+  int64_t pitch;
+  int count;
+  bool any;
+  if (images) {
+    const int64_t i = (int64_t)job * side + (threadIdx.x & (side - 1)), image = i / C4;
+    any = i < (int64_t)p.images * C4;
+    count = p.units_per_gate;
+    in = reinterpret_cast<const float4*>(p.unit_sums) + image * count * C4 + (i - image * C4);
+    out = reinterpret_cast<float4*>(p.dgate) + i;
+    pitch = C4;
+  } else {
+    const int which = blockIdx.x / groups, i = (blockIdx.x - which * groups) * side + (threadIdx.x & (side - 1));
+    any = i < C4;
+    count = p.blocks;
+    in = reinterpret_cast<const float4*>(p.block_sums) + (int64_t)p.kind[which] * C4 + i;
+    out = reinterpret_cast<float4*>(p.out[which]) + i;
+    pitch = (int64_t)kSums * C4;
   }
-  job -= groups * p.wanted;
-  const int64_t i = (int64_t)job * 1024 + threadIdx.x;
-  const int C4 = p.C / 4;
-  if (i >= (int64_t)p.images * C4) return;
-  const int64_t image = i / C4;
-  const float4* in = reinterpret_cast<const float4*>(p.unit_sums) + image * p.units_per_gate * C4 + (i - image * C4);
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-  for (int u = 0; u < p.units_per_gate; ++u) {
-    const float4 v = in[(int64_t)u * C4];
+  const auto add = [&](const float4& v) {
     s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  };
+  if (!any) count = 0;
+  for (int u = r; u < count; u += 8 << shift) {  // eight loads under way
+    float4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = u + (k << shift) < count ? in[(u + (k << shift)) * pitch] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add(v[k]);
   }
-  reinterpret_cast<float4*>(p.dgate)[i] = s;
+  if (shift != 0) {
+    for (int o = 16; o >= side; o >>= 1)  // the same columns in a warp
+      add(make_float4(__shfl_xor_sync(0xFFFFFFFFu, s.x, o), __shfl_xor_sync(0xFFFFFFFFu, s.y, o), __shfl_xor_sync(0xFFFFFFFFu, s.z, o),
+                      __shfl_xor_sync(0xFFFFFFFFu, s.w, o)));
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if (r != 0) return;
+    const int next = side < 32 ? 32 : side;
+#pragma unroll 8
+    for (int k = threadIdx.x + next; k < 1024; k += next) add(part[k]);
+  }
+  if (any) *out = s;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -864,7 +881,13 @@ cudaError_t launch_resnorm_backward(const ssconv_resnorm_t& d, const ResnormTens
   f.units_per_gate = c.units_per_gate;
   f.images = c.image_gates && c.units_per_gate > 1 && g.dgate != nullptr ? c.images : 0;
   f.dgate = g.dgate;
-  const int64_t blocks = (int64_t)((d.C + 31) / 32) * f.wanted + ((int64_t)f.images * (d.C / 4) + 1023) / 1024;
+  const int64_t C4 = d.C / 4;
+  const auto jobs = [](int64_t columns, int shift) { return (columns + (1024 >> shift) - 1) >> (10 - shift); };
+  // the images' units: up to eight rows per thread; the blocks' sums: as many threads as make for two blocks per SM
+  while (f.image_shift < 5 && (8 << f.image_shift) < c.units_per_gate) ++f.image_shift;
+  f.block_shift = 5;
+  while (f.block_shift < 7 && jobs(C4, f.block_shift + 1) * f.wanted <= 2 * device_sms()) ++f.block_shift;
+  const int64_t blocks = jobs(C4, f.block_shift) * f.wanted + jobs(f.images * C4, f.image_shift);
   if (blocks == 0) return cudaSuccess;
   count_launch();
   return launch_dependent(resnorm_finish_kernel, (unsigned)blocks, 1024, st, f);
