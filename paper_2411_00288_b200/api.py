@@ -949,7 +949,7 @@ def ssconv_residual_norm_backward(desc: ResNorm, x: torch.Tensor, b: torch.Tenso
                                   pre_gamma: Optional[torch.Tensor] = None, pre_beta: Optional[torch.Tensor] = None,
                                   ws: Optional[torch.Tensor] = None, stream=None) -> ResNormGrads:
     """Gradients from dh and dy (bf16 like x; dh may be None) and the forward call's inputs and stats: dx, db bf16, the others
-    fp32 and of their inputs' shapes, one for each gate, gamma and beta that is given."""
+    fp32 and of their inputs' shapes, one for each gate, gamma and beta that is given (parts of one allocation)."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return ssconv_residual_norm_backward(desc, x, b, stats, dh, dy, gate, post_gamma, post_beta, pre_gamma, pre_beta, ws)

@@ -179,6 +179,28 @@ at::Tensor given_or_new(PyObject* o, at::IntArrayRef shape, at::ScalarType type,
   if (o != Py_None) return as_tensor(o);
   return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
 }
+// New fp32 tensors shaped like those of `like` that are not None, one after the other in one allocation (extents: multiples of 8).
+template <size_t N>
+void allocate_like(PyObject* const* like, at::Tensor (&out)[N], const at::Tensor& beside) {
+  int64_t total = 0;
+  bool any = false;
+  for (size_t i = 0; i < N; ++i) {
+    if (like[i] == Py_None) continue;
+    any = true;
+    total += as_tensor(like[i]).numel();
+  }
+  if (!any) return;
+  const at::Tensor all = at::detail::empty_cuda({total}, at::kFloat, beside.device(), std::nullopt);
+  int64_t from = 0;
+  for (size_t i = 0; i < N; ++i) {
+    if (like[i] == Py_None) continue;
+    const at::Tensor& shape = as_tensor(like[i]);
+    out[i] = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+    out[i].unsafeGetTensorImpl()->set_storage_offset(from);
+    out[i].unsafeGetTensorImpl()->set_sizes_contiguous(shape.sizes());
+    from += shape.numel();
+  }
+}
 void* address(const at::Tensor& t) { return t.numel() != 0 ? t.mutable_data_ptr() : nullptr; }
 
 // (status, results...): what a call gives back to its Python function.
@@ -379,8 +401,8 @@ PyObject* residual_norm_backward(PyObject* const* a) {
   const void* dy = expect(a[10], "dy", at::kBFloat16, elements(d));
   at::Tensor dx = given_or_new(Py_None, x.sizes(), at::kBFloat16, x), db = given_or_new(Py_None, x.sizes(), at::kBFloat16, x), sums[5], ws;
   float* out[5];
+  allocate_like(a + 3, sums, x);
   for (int i = 0; i < 5; ++i) {
-    if (a[3 + i] != Py_None) sums[i] = given_or_new(Py_None, as_tensor(a[3 + i]).sizes(), at::kFloat, x);
     out[i] = sums[i].defined() ? static_cast<float*>(address(sums[i])) : nullptr;
   }
   if (a[11] != Py_None) {

@@ -278,3 +278,29 @@ def test_refuses_overlaps_of_what_is_written():
         a = list(base)
         a[6] = a[other] + ends[other] - 4
         assert f.ssconv_forward_dense_mxfp4(desc, *a, None) == BAD, other
+
+
+@pytest.mark.parametrize("order", ["ascending", "descending", "interleaved", "shuffled"])
+def test_adamw_finds_one_overlap_among_many_tensors(order):
+    """4 lists of 97 tensors, 4096 bytes apart, of which one reaches into its neighbour: refused wherever it is."""
+    lists, count = 4, 97
+    at = [(1 << 30) + 4096 * i for i in range(lists * count)]
+    if order == "interleaved":
+        rows = [at[k::lists] for k in range(lists)]
+    else:
+        if order == "descending":
+            at.reverse()
+        elif order == "shuffled":
+            at = [at[(37 * i + 11) % len(at)] for i in range(len(at))]
+        rows = [at[k * count:(k + 1) * count] for k in range(lists)]
+    assert len({a for r in rows for a in r}) == lists * count
+    f = api.lib().ssconv_adamw_multi
+    for which in range(lists):
+        for i in (0, 1, 48, count - 1):
+            moved = [list(r) for r in rows]
+            step = 4096 if moved[which][i] + 4096 in at else -4096
+            if which == 1 and moved[which][i] + step in rows[1]:         # (two gradients, both only read)
+                continue
+            moved[which][i] += step * (4096 - 16) // 4096
+            theta, g, m, v = _arrays(*moved)
+            assert f(theta, g, m, v, _counts(*[1024 - 4] * count), None, count, 1, 1.0, 0.9, 0.999, 1e-8, 0.0, None, 1.0, None) == BAD
