@@ -968,7 +968,7 @@ def ssconv_sizes_mxfp4(rows: int, C: int) -> Tuple[int, int]:
 
 def ssconv_quantize_mxfp4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """(codes, scales) uint8 of bf16 x [..., C]: e2m1 elements, one power of two per 32 channels; scales in the tile order that
-    ssconv_forward_dense_mxfp4 reads.  Weights [C_out, C_in] are quantised by the same call."""
+    ssconv_forward_dense_mxfp4 reads; new ones are parts of one allocation.  Weights [C_out, C_in] are quantised by the same call."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return ssconv_quantize_mxfp4(x, codes, scales)

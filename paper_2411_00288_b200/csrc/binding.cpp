@@ -179,6 +179,13 @@ at::Tensor given_or_new(PyObject* o, at::IntArrayRef shape, at::ScalarType type,
   if (o != Py_None) return as_tensor(o);
   return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
 }
+// A part of a contiguous tensor's allocation, from one of its elements on.
+at::Tensor part_of(const at::Tensor& all, int64_t from, at::IntArrayRef shape) {
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+  t.unsafeGetTensorImpl()->set_storage_offset(from);
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+  return t;
+}
 // New fp32 tensors shaped like those of `like` that are not None, one after the other in one allocation (extents: multiples of 8).
 template <size_t N>
 void allocate_like(PyObject* const* like, at::Tensor (&out)[N], const at::Tensor& beside) {
@@ -195,9 +202,7 @@ void allocate_like(PyObject* const* like, at::Tensor (&out)[N], const at::Tensor
   for (size_t i = 0; i < N; ++i) {
     if (like[i] == Py_None) continue;
     const at::Tensor& shape = as_tensor(like[i]);
-    out[i] = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
-    out[i].unsafeGetTensorImpl()->set_storage_offset(from);
-    out[i].unsafeGetTensorImpl()->set_sizes_contiguous(shape.sizes());
+    out[i] = part_of(all, from, shape.sizes());
     from += shape.numel();
   }
 }
@@ -440,7 +445,16 @@ PyObject* quantize_mxfp4(PyObject* const* a) {
   if (sized != SSCONV_OK) return results(sized, at::Tensor(), at::Tensor());
   expect(a[1], "codes", at::kByte, (int64_t)n_codes);
   expect(a[2], "scales", at::kByte, (int64_t)n_scales);
-  const at::Tensor codes = given_or_new(a[1], with_last(x, (C + 31) / 32 * 16), at::kByte, x), scales = given_or_new(a[2], {(int64_t)n_scales}, at::kByte, x);
+  const std::vector<int64_t> shape = with_last(x, (C + 31) / 32 * 16);
+  at::Tensor codes, scales;
+  if (a[1] == Py_None && a[2] == Py_None) {  // both in one allocation: one is of no use without the other
+    const at::Tensor all = at::detail::empty_cuda({(int64_t)(n_codes + n_scales)}, at::kByte, x.device(), std::nullopt);
+    codes = part_of(all, 0, shape);
+    scales = part_of(all, (int64_t)n_codes, {(int64_t)n_scales});
+  } else {
+    codes = given_or_new(a[1], shape, at::kByte, x);
+    scales = given_or_new(a[2], {(int64_t)n_scales}, at::kByte, x);
+  }
   void* stream = current_stream();
   const int32_t rc = without_gil([&] { return ssconv_quantize_mxfp4(px, rows, (int32_t)C, address(codes), address(scales), stream); });
   return results(rc, codes, scales);
