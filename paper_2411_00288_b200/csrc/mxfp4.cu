@@ -174,49 +174,57 @@ struct MxParams {
 constexpr uint32_t kDescHiSw64 = (512u >> 4) | (1u << 14) | (4u << 29);
 constexpr uint32_t kDescHiSw32 = (256u >> 4) | (1u << 14) | (6u << 29);
 
+// The roles' warps go on in lock step, and one lane issues.  It is elected once: elected for each instruction, the same instructions
+// kept the tensor cores and copies waiting (us before and after, 8192 x 4096 -> 4096 70.7 / 63.7, 16 x 4096 -> 4096 8.9 / 7.6, 25088 x
+// 1536 -> 384 14.3 / 13.3).  The commits elect by themselves: with all 32 lanes asking it is always the same lane.
+__device__ __forceinline__ uint32_t elected() {
+  uint32_t lead;
+  asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(lead));
+  return lead;
+}
 // 32x128b.warpx4: 512 bytes (32 rows of 16, unswizzled) into 4 TMEM columns, the same 32 lanes in each of the four quarters.
-__device__ __forceinline__ void tc_cp_32x128b_x4_w(uint32_t dst_tmem, uint32_t src_lo) {
+__device__ __forceinline__ void tc_cp_32x128b_x4(uint32_t dst_tmem, uint32_t src_lo, uint32_t lead) {
   asm volatile(
       "{\n\t.reg .pred e;\n\t.reg .b64 ds;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 e, %3, 0;\n\t"
       "mov.b64 ds, {%1, %2};\n\t"
       "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], ds;\n\t}"
-      ::"r"(dst_tmem), "r"(src_lo), "r"(kDescHiNoSwizzle128)
+      ::"r"(dst_tmem), "r"(src_lo), "r"(kDescHiNoSwizzle128), "r"(lead)
       : "memory");
 }
 // D[128 x N] (+)= A[128 x 64] B[N x 64]^T, e2m1 operands with one e8m0 scale per 32 elements of a row, taken from TMEM.
-__device__ __forceinline__ void tc_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
-                                              uint32_t sfb, uint32_t accumulate) {
+__device__ __forceinline__ void tc_mma_mxf4(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
+                                              uint32_t sfb, uint32_t accumulate, uint32_t lead) {
   asm volatile(
       "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 e, %8, 0;\n\t"
       "mov.b64 da, {%1, %7};\n\t"
       "mov.b64 db, {%2, %7};\n\t"
       "setp.ne.b32 p, %6, 0;\n\t"
       "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(desc_hi)
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(desc_hi), "r"(lead)
       : "memory");
 }
 // The same two for a pair: both blocks' scales into their own TMEM; 256 rows of A, the blocks' halves of B one after the other.
-__device__ __forceinline__ void tc2_cp_32x128b_x4_w(uint32_t dst_tmem, uint32_t src_lo) {
+__device__ __forceinline__ void tc2_cp_32x128b_x4(uint32_t dst_tmem, uint32_t src_lo, uint32_t lead) {
   asm volatile(
       "{\n\t.reg .pred e;\n\t.reg .b64 ds;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 e, %3, 0;\n\t"
       "mov.b64 ds, {%1, %2};\n\t"
       "@e tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], ds;\n\t}"
-      ::"r"(dst_tmem), "r"(src_lo), "r"(kDescHiNoSwizzle128)
+      ::"r"(dst_tmem), "r"(src_lo), "r"(kDescHiNoSwizzle128), "r"(lead)
       : "memory");
 }
-__device__ __forceinline__ void tc2_mma_mxf4_w(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
-                                               uint32_t sfb, uint32_t accumulate) {
+__device__ __forceinline__ void tc2_mma_mxf4(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
+                                               uint32_t sfb, uint32_t accumulate, uint32_t lead) {
   asm volatile(
       "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 e, %8, 0;\n\t"
       "mov.b64 da, {%1, %7};\n\t"
       "mov.b64 db, {%2, %7};\n\t"
       "setp.ne.b32 p, %6, 0;\n\t"
       "@e tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(desc_hi)
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(desc_hi), "r"(lead)
       : "memory");
 }
 // Instruction descriptor of kind::mxf4: bits 4-5 and 29-30 which of a row's scales in its TMEM word (0 or 2: the first two or the
@@ -242,6 +250,14 @@ __device__ __forceinline__ void tc_wait_ld_x16(uint32_t (&r)[16]) {
                  "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
                :
                : "memory");
+}
+
+// A load whose completion is signalled on an mbarrier of either block of a pair, by one thread.
+__device__ __forceinline__ void tma2_load_2d_a(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y)
+      : "memory");
 }
 
 template <int BN, bool PAIR, int ACT>
@@ -316,6 +332,7 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
     const uint32_t full0 = PAIR ? map_to_cta(smem_u32(full), 0) : smem_u32(full);
     uint32_t s = 0, phase = 0;
     bool ok = true;
+    const uint32_t lead = elected();
     for (int t = first_tile; t < tiles && ok; t += tile_step) {
       const int mt = t / p.n_tiles, n = t - mt * p.n_tiles, m = PAIR ? 2 * mt + (int)rank : mt;
       const int first = n * BN >> 7;
@@ -330,23 +347,25 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
         const uint32_t bar = full0 + 8 * s, sc = s0 + s * T::kBytesScales;
         const bool tail = kb == stages - 1;
         const uint32_t codes = (tail ? p.tail_bytes : 128) * (p.x_rows + p.w_rows);
-        if constexpr (PAIR) {
-          // (two images per copy, whether there is a second one or not: what it brings instead is not used)
-          if (rank == 0) mbar_expect_tx_w(smem_u32(full) + 8 * s, 2 * (codes + T::kBytesScales));
-          tma2_load_2d_w(a0 + s * T::kBytesA, tail ? &tm_x_tail : &tm_x, bar, kb * 128, m * 128);
-          tma2_load_2d_w(b0 + s * T::kBytesB, tail ? &tm_w_tail : &tm_w, bar, kb * 128, n * BN + (int)rank * (BN / 2));
-          tma2_load_2d_w(sc, &tm_x_scales, bar, 0, m * p.chunks + 2 * kb);
+        if (lead) {
+          if constexpr (PAIR) {
+            // (two images per copy, whether there is a second one or not: what it brings instead is not used)
+            if (rank == 0) mbar_expect_tx_a(smem_u32(full) + 8 * s, 2 * (codes + T::kBytesScales));
+            tma2_load_2d_a(a0 + s * T::kBytesA, tail ? &tm_x_tail : &tm_x, bar, kb * 128, m * 128);
+            tma2_load_2d_a(b0 + s * T::kBytesB, tail ? &tm_w_tail : &tm_w, bar, kb * 128, n * BN + (int)rank * (BN / 2));
+            tma2_load_2d_a(sc, &tm_x_scales, bar, 0, m * p.chunks + 2 * kb);
 #pragma unroll
-          for (int i = 0; i < T::kScaleTiles; ++i) tma2_load_2d_w(sc + 1024 * (1 + i), &tm_w_scales, bar, 0, (first + i) * p.chunks + 2 * kb);
-        } else {
-          const uint32_t part = min(2, p.chunks - 2 * kb) * kMxImageBytes;
-          mbar_expect_tx_w(bar, codes + part * (1 + images));
-          tma_load_2d_w(a0 + s * T::kBytesA, tail ? &tm_x_tail : &tm_x, bar, kb * 128, m * 128);
-          tma_load_2d_w(b0 + s * T::kBytesB, tail ? &tm_w_tail : &tm_w, bar, kb * 128, n * BN);
-          bulk_load_w(sc, xs + kb * 2 * kMxImageBytes, part, bar);
+            for (int i = 0; i < T::kScaleTiles; ++i) tma2_load_2d_a(sc + 1024 * (1 + i), &tm_w_scales, bar, 0, (first + i) * p.chunks + 2 * kb);
+          } else {
+            const uint32_t part = min(2, p.chunks - 2 * kb) * kMxImageBytes;
+            mbar_expect_tx_a(bar, codes + part * (1 + images));
+            tma_load_2d_a(a0 + s * T::kBytesA, tail ? &tm_x_tail : &tm_x, bar, kb * 128, m * 128);
+            tma_load_2d_a(b0 + s * T::kBytesB, tail ? &tm_w_tail : &tm_w, bar, kb * 128, n * BN);
+            bulk_load_a(sc, xs + kb * 2 * kMxImageBytes, part, bar);
 #pragma unroll
-          for (int i = 0; i < T::kScaleTiles; ++i)
-            if (i < images) bulk_load_w(sc + 1024 * (1 + i), ws + ((int64_t)i * p.chunks + 2 * kb) * kMxImageBytes, part, bar);
+            for (int i = 0; i < T::kScaleTiles; ++i)
+              if (i < images) bulk_load_a(sc + 1024 * (1 + i), ws + ((int64_t)i * p.chunks + 2 * kb) * kMxImageBytes, part, bar);
+          }
         }
         if (++s == T::kStages) {
           s = 0;
@@ -360,6 +379,7 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
     const uint32_t a0 = desc_lo(smem_u32(ring_a)), b0 = desc_lo(smem_u32(ring_b));
     const uint32_t scaled0 = smem_u32(scaled), empty0 = smem_u32(empty), acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
     uint32_t s = 0, phase = 0, buf = 0, acc_phase = 0, ready = 0;
+    const uint32_t lead = elected();
     bool ok = true;
     for (int t = first_tile; t < tiles && ok; t += tile_step) {
       // tiles that start inside an image take its later columns
@@ -385,9 +405,9 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
             const uint32_t idesc = make_idesc_mxf4(PAIR ? 256 : 128, BN, 2 * (k & 1));
             const uint32_t sa = sfa + 4 * (k >> 1), sb = sfb + 4 * T::kScaleTiles * (k >> 1);
             if (PAIR)
-              tc2_mma_mxf4_w(d, a_lo + 2 * k, b_lo + 2 * k, desc_hi, idesc, sa, sb, (kb | k) != 0);
+              tc2_mma_mxf4(d, a_lo + 2 * k, b_lo + 2 * k, desc_hi, idesc, sa, sb, (kb | k) != 0, lead);
             else
-              tc_mma_mxf4_w(d, a_lo + 2 * k, b_lo + 2 * k, desc_hi, idesc, sa, sb, (kb | k) != 0);
+              tc_mma_mxf4(d, a_lo + 2 * k, b_lo + 2 * k, desc_hi, idesc, sa, sb, (kb | k) != 0, lead);
           }
         if (PAIR)
           tc2_commit_both_w(empty0 + 8 * s);
@@ -408,10 +428,10 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
   } else if (warp == T::kScaler) {
    if (rank == 0) {
     // ---------------------------------------------------------------- scales into TMEM
-    // (by a warp of its own: an issuer takes some 60 cycles per tcgen05 instruction and 200 per wait, and there are six of these
-    // beside four MMAs)
+    // (by a warp of its own: waits and tcgen05 instructions cost an issuer time, and there are six of these beside four MMAs)
     const uint32_t s0 = desc_lo(smem_u32(ring_s)), full0 = smem_u32(full), scaled0 = smem_u32(scaled);
     uint32_t s = 0, phase = 0, ready = 0;
+    const uint32_t lead = elected();
     bool ok = true;
     for (int t = first_tile; t < tiles && ok; t += tile_step) {
       for (int kb = 0; kb < stages; ++kb) {
@@ -424,11 +444,11 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
         ready = mbar_test_a(full0 + 8 * next, next_phase);
         const uint32_t sfa = tmem + 2 * BN + s * T::kScaleColumns, sfb = sfa + 8, src = s0 + s * (T::kBytesScales >> 4);
         const bool second = p.steps - 4 * kb > 2;
-        const auto copy = [](uint32_t to, uint32_t from) {
+        const auto copy = [lead](uint32_t to, uint32_t from) {
           if (PAIR)
-            tc2_cp_32x128b_x4_w(to, from);
+            tc2_cp_32x128b_x4(to, from, lead);
           else
-            tc_cp_32x128b_x4_w(to, from);
+            tc_cp_32x128b_x4(to, from, lead);
         };
         copy(sfa, src);
 #pragma unroll
@@ -657,9 +677,10 @@ int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const 
   const int act = activation_of(d.flags);
   // The width, by cycles (fitted to 401408 x 96 -> 384 and 8192 x 4096 -> 4096): a tile takes the longer of filling shared memory and
   // of its epilogue, and the first of the one and the last of the other are not hidden.  Shared memory fills at 50 bytes per cycle and
-  // SM, 12 TB/s out of L2 in all, which is what long K is bound by (with three of four MMAs left out 8192 x 4096 -> 4096 still took 62 us
-  // of 72).  Pairs halve the weights' share of it, at a lower rate.  us at 192 / 128 / 64 columns / 192 on pairs: 401408 x 96 -> 384 74 /
-  // 76 / 93, 8192 x 4096 -> 4096 77 / 90 / 162 / 72, 25088 x 1536 -> 384 14.4 / 16.4 / 24.7 / 15.1, 3136 x 256 -> 1024 8.1 / 6.3 / 8.3.
+  // SM, 12 TB/s out of L2 in all, which is what long K is bound by (with three of four MMAs left out 8192 x 4096 -> 4096 took 62 us, with
+  // all of them 63.7).  Pairs halve the weights' share of it, at a lower rate.  us at 192 / 128 / 64 columns / 192 on pairs: 401408 x 96
+  // -> 384 71.5 / 74.8 / 87.5 / 99.8, 8192 x 4096 -> 4096 69.8 / 76.9 / 126 / 63.7, 25088 x 1536 -> 384 13.3 / 12.7 / 18.8 / 14.4, 1024 x
+  // 4096 -> 4096 17.4 / 14.4 / 21.6 / 16.5, 512 x 1024 -> 1024 7.2 / 6.2 / 5.2 / 7.7.
   const int mx_stages = (gx.blocks + 7) / 8;
   int bn = 0;
   bool pair = false;
