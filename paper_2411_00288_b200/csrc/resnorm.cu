@@ -158,35 +158,51 @@ struct TeamSum {
 
 // Mean (0 for RMS) and 1 / deviation of a row; two passes over the registers, so that a mean far from zero costs no digits.  (A
 // block's warps could put sums about their own means together with one barrier instead of two: 3000 x 4096 78 us instead of 40.)
-template <int LANES, int V, bool BLOCK>
-__device__ __forceinline__ void row_statistics(const Pair (&v)[V][4], const bool (&live)[V], bool layer, float inv_c, float eps,
-                                               TeamSum<LANES, BLOCK>& sum, float& mean, float& rstd) {
-  mean = 0.0f;
+template <int LANES, int V, bool BLOCK, int R>
+__device__ __forceinline__ void row_statistics(const Pair (&v)[R][V][4], const bool (&live)[V], bool layer, float inv_c, float eps,
+                                               TeamSum<LANES, BLOCK>& sum, float (&mean)[R], float (&rstd)[R]) {
+  const auto sums = [&](float(&a)[R]) {
+    if constexpr (R == 1)
+      sum(a[0]);
+    else
+      sum(a[0], a[1]);
+  };
+#pragma unroll
+  for (int i = 0; i < R; ++i) mean[i] = 0.0f;
   if (layer) {
-    Pair s = v[0][0];
 #pragma unroll
-    for (int k = 0; k < V; ++k)
+    for (int i = 0; i < R; ++i) {
+      Pair s = v[i][0][0];
 #pragma unroll
-      for (int j = k == 0 ? 1 : 0; j < 4; ++j) s = add2(s, v[k][j]);  // (zeros in pieces past the row)
-    mean = sum_of(s);
-    sum(mean);
-    mean *= inv_c;
-  }
-  Pair q = 0;
-  const Pair less = both(-mean);
+      for (int k = 0; k < V; ++k)
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    Pair r = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const Pair d = add2(v[k][j], less);
-      r = fma2(d, d, r);
+        for (int j = k == 0 ? 1 : 0; j < 4; ++j) s = add2(s, v[i][k][j]);  // (zeros in pieces past the row)
+      mean[i] = sum_of(s);
     }
-    q = add2(q, live[k] ? r : 0ull);
+    sums(mean);
+#pragma unroll
+    for (int i = 0; i < R; ++i) mean[i] *= inv_c;
   }
-  float t = sum_of(q);
-  sum(t);
-  rstd = rsqrtf(t * inv_c + eps);
+  float t[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    Pair q = 0;
+    const Pair less = both(-mean[i]);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      Pair r = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const Pair d = add2(v[i][k][j], less);
+        r = fma2(d, d, r);
+      }
+      q = add2(q, live[k] ? r : 0ull);
+    }
+    t[i] = sum_of(q);
+  }
+  sums(t);
+#pragma unroll
+  for (int i = 0; i < R; ++i) rstd[i] = rsqrtf(t[i] * inv_c + eps);
 }
 
 constexpr int kCrewThreads = 256;  // of a block whose teams are parts of warps
@@ -222,7 +238,7 @@ struct RowRing {
 };
 constexpr int kForwardDepth = 3;
 __host__ __device__ constexpr int backward_depth(int V) { return V == 1 ? 3 : 2; }
-constexpr int forward_smem(int V, int threads) { return kForwardDepth * 2 * V * 16 * threads; }
+constexpr int forward_smem(int V, int threads, int R) { return kForwardDepth * 2 * V * R * 16 * threads; }
 constexpr int backward_smem(int V, int threads) { return backward_depth(V) * (4 * V + 1) * 16 * threads; }
 constexpr int kMostSlots = 160 * 1024;  // bytes of any block's slots
 
@@ -234,7 +250,7 @@ struct ForwardParams {
   float scale, eps;
 };
 
-template <int LANES, int V, bool BLOCK, bool POST, bool PRE>
+template <int LANES, int V, bool BLOCK, bool POST, bool PRE, int R = 1>
 __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(const ForwardParams p) {
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ __align__(256) float scratch[64];
@@ -247,7 +263,7 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
   const float inv_c = 1.0f / (float)(8 * C8);
   TeamSum<LANES, BLOCK> sum;
   sum.begin(scratch);
-  RowRing<2 * V, kForwardDepth, BLOCK> ring(slots);
+  RowRing<2 * V * R, kForwardDepth, BLOCK> ring(slots);
   bool own[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) own[k] = sub + k * run < C8;
@@ -263,14 +279,16 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
   int coming_row = row;
   const auto fetch = [&] {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const bool mine = coming_row < last && own[k];
-      const int64_t at = mine ? coming + k * 16 * run : 0;
-      ring.fetch(2 * k, static_cast<const uint8_t*>(p.t.x) + at, mine ? 16u : 0u);
-      ring.fetch(2 * k + 1, static_cast<const uint8_t*>(p.t.b) + at, mine ? 16u : 0u);
-    }
-    coming += stride;
-    coming_row += kTeams;
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const bool mine = coming_row + i < last && own[k];
+        const int64_t at = mine ? coming + i * stride + k * 16 * run : 0;
+        ring.fetch(2 * (i * V + k), static_cast<const uint8_t*>(p.t.x) + at, mine ? 16u : 0u);
+        ring.fetch(2 * (i * V + k) + 1, static_cast<const uint8_t*>(p.t.b) + at, mine ? 16u : 0u);
+      }
+    coming += R * stride;
+    coming_row += R * kTeams;
     ring.next_row();
   };
   grid_dependency_wait();
@@ -285,41 +303,47 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
   if (PRE) pre_beta.set(p.t.pre_beta, 0.0f, sub, run, own);
   int gates_end = p.rows_per_gate > 0 ? 0 : p.rows;  // the first row with other gates
   const Pair scale = both(p.scale);
-  for (; row - team < last; row += kTeams, here += stride) {
-    const bool there = row < last;
+  for (; row - team < last; row += R * kTeams, here += R * stride) {
     fetch();
     ring.wait();
-    Pair bv[V][4], hv[V][4];
+    Pair bv[R][V][4], hv[R][V][4];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      unpack8(ring.read(2 * k), hv[k]);
-      unpack8(ring.read(2 * k + 1), bv[k]);
-    }
-    float4 stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (POST) row_statistics<LANES, V, BLOCK>(bv, own, p.post_layer, inv_c, p.eps, sum, stats.x, stats.y);
-    if (there && row >= gates_end) {
-      const int image = row / p.rows_per_gate;
-      gates_end = (int)min((int64_t)p.rows, (int64_t)(image + 1) * p.rows_per_gate);
-      gates.set(p.t.gate != nullptr ? p.t.gate + (int64_t)image * (8 * C8) : p.t.gate, 1.0f, sub, run, own);
-    }
+    for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const int piece = sub + k * run;
-      Pair g[4];
-      gates.get(k, piece, own[k], g);
-      if (POST) {
-        Pair a[4], c[4];
-        post_gamma.get(k, piece, own[k], a);
-        post_beta.get(k, piece, own[k], c);
+      for (int k = 0; k < V; ++k) {
+        unpack8(ring.read(2 * (i * V + k)), hv[i][k]);
+        unpack8(ring.read(2 * (i * V + k) + 1), bv[i][k]);
+      }
+    float post_mean[R] = {}, post_rstd[R] = {}, pre_mean[R] = {}, pre_rstd[R] = {};
+    if (POST) row_statistics<LANES, V, BLOCK, R>(bv, own, p.post_layer, inv_c, p.eps, sum, post_mean, post_rstd);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) bv[k][j] = fma2(mul2(add2(bv[k][j], both(-stats.x)), both(stats.y)), a[j], c[j]);
+    for (int i = 0; i < R; ++i) {
+      const bool there = row + i < last;
+      if (there && row + i >= gates_end) {
+        const int image = (row + i) / p.rows_per_gate;
+        gates_end = (int)min((int64_t)p.rows, (int64_t)(image + 1) * p.rows_per_gate);
+        gates.set(p.t.gate != nullptr ? p.t.gate + (int64_t)image * (8 * C8) : p.t.gate, 1.0f, sub, run, own);
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) hv[k][j] = fma2(g[j], bv[k][j], mul2(scale, hv[k][j]));
-      if (there && own[k] && p.t.h != nullptr) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.t.h) + here + k * 16 * run) = pack8(hv[k]);
+      for (int k = 0; k < V; ++k) {
+        const int piece = sub + k * run;
+        Pair g[4];
+        gates.get(k, piece, own[k], g);
+        if (POST) {
+          Pair a[4], c[4];
+          post_gamma.get(k, piece, own[k], a);
+          post_beta.get(k, piece, own[k], c);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) bv[i][k][j] = fma2(mul2(add2(bv[i][k][j], both(-post_mean[i])), both(post_rstd[i])), a[j], c[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) hv[i][k][j] = fma2(g[j], bv[i][k][j], mul2(scale, hv[i][k][j]));
+        if (there && own[k] && p.t.h != nullptr)
+          *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.t.h) + here + i * stride + k * 16 * run) = pack8(hv[i][k]);
+      }
     }
     if (PRE) {
-      row_statistics<LANES, V, BLOCK>(hv, own, p.pre_layer, inv_c, p.eps, sum, stats.z, stats.w);
+      row_statistics<LANES, V, BLOCK, R>(hv, own, p.pre_layer, inv_c, p.eps, sum, pre_mean, pre_rstd);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const int piece = sub + k * run;
@@ -327,11 +351,18 @@ __global__ void __launch_bounds__(BLOCK ? 512 : kCrewThreads) resnorm_kernel(con
         pre_gamma.get(k, piece, own[k], a);
         pre_beta.get(k, piece, own[k], c);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) hv[k][j] = fma2(mul2(add2(hv[k][j], both(-stats.z)), both(stats.w)), a[j], c[j]);
-        if (there && own[k]) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.t.y) + here + k * 16 * run) = pack8(hv[k]);
+        for (int i = 0; i < R; ++i) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) hv[i][k][j] = fma2(mul2(add2(hv[i][k][j], both(-pre_mean[i])), both(pre_rstd[i])), a[j], c[j]);
+          if (row + i < last && own[k]) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.t.y) + here + i * stride + k * 16 * run) = pack8(hv[i][k]);
+        }
       }
     }
-    if (sub == 0 && there && p.t.stats != nullptr) reinterpret_cast<float4*>(p.t.stats)[row] = stats;
+    if (sub == 0 && p.t.stats != nullptr) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (row + i < last) reinterpret_cast<float4*>(p.t.stats)[row + i] = make_float4(post_mean[i], post_rstd[i], pre_mean[i], pre_rstd[i]);
+    }
   }
 }
 
@@ -731,7 +762,7 @@ int resident_blocks(const void* kernel, int threads, int smem) {
   return blocks;
 }
 
-static_assert(forward_smem(2, 512) <= kMostSlots && forward_smem(3, 256) <= kMostSlots && backward_smem(1, 512) <= kMostSlots && backward_smem(2, 512) <= kMostSlots, "");
+static_assert(forward_smem(1, 512, 2) <= kMostSlots && forward_smem(2, 512, 1) <= kMostSlots && forward_smem(3, 256, 1) <= kMostSlots && backward_smem(1, 512) <= kMostSlots && backward_smem(2, 512) <= kMostSlots, "");
 
 // The kernel of a team.
 #define SSCONV_LANES_KERNEL(kernel, V)                        \
@@ -744,7 +775,8 @@ static_assert(forward_smem(2, 512) <= kMostSlots && forward_smem(3, 256) <= kMos
     default: return kernel<32, V, false, POST, PRE>;          \
   }
 template <bool POST, bool PRE>
-void (*forward_kernel(const Team& t))(ForwardParams) {
+void (*forward_kernel(const Team& t, int R))(ForwardParams) {
+  if (t.block && R == 2) return resnorm_kernel<32, 1, true, POST, PRE, 2>;
   if (t.block) return t.V == 1 ? resnorm_kernel<32, 1, true, POST, PRE> : resnorm_kernel<32, 2, true, POST, PRE>;
   if (t.V == 1) SSCONV_LANES_KERNEL(resnorm_kernel, 1)
   if (t.V == 2) SSCONV_LANES_KERNEL(resnorm_kernel, 2)
@@ -811,19 +843,28 @@ cudaError_t launch_resnorm(const ssconv_resnorm_t& d, const ResnormTensors& t, c
   const int C8 = d.C / 8;
   const Team team = team_for(C8, 3, d.rows);
   const bool post = d.post != SSCONV_NORM_NONE, pre = d.pre != SSCONV_NORM_NONE && t.y != nullptr;
-  const auto kernel = post ? (pre ? forward_kernel<true, true>(team) : forward_kernel<true, false>(team))
-                           : (pre ? forward_kernel<false, true>(team) : forward_kernel<false, false>(team));
-  const int smem = forward_smem(team.V, team.threads);
+  const auto kernel_of = [&](int rows) {
+    return post ? (pre ? forward_kernel<true, true>(team, rows) : forward_kernel<true, false>(team, rows))
+                : (pre ? forward_kernel<false, true>(team, rows) : forward_kernel<false, false>(team, rows));
+  };
+  const auto resident = [&](int rows) {
+    return resident_blocks((const void*)kernel_of(rows), team.threads, forward_smem(team.V, team.threads, rows));
+  };
+  // Blocks take two rows at a time, whose sums share barriers, where as many blocks with two rows as with one fit an SM.  us with
+  // one / two, both norms: 9000 x 4096 97 / 83, 3500 x 3584 39 / 33, 6000 x 2048 31 / 28; where fewer fit: 5000 x 2504 33 / 38.
+  const int R = team.block && team.V == 1 && d.rows > 8 * (int64_t)device_sms() && resident(2) >= resident(1) ? 2 : 1;
+  const auto kernel = kernel_of(R);
+  const int smem = forward_smem(team.V, team.threads, R);
   const int teams = team.block ? 1 : 32 / team.lanes, crews_per_block = team.block ? 1 : team.threads / 32;
-  const int64_t most = (int64_t)device_sms() * resident_blocks((const void*)kernel, team.threads, smem) * crews_per_block;
+  const int64_t most = (int64_t)device_sms() * resident(R) * crews_per_block;
   if (most == 0) return cudaErrorUnknown;
-  const int64_t turns = (d.rows + most * teams - 1) / (most * teams);
+  const int64_t turns = (d.rows + most * teams * R - 1) / (most * teams * R);
   ForwardParams p = {};
   p.t = t;
   p.rows = (int)d.rows;
   p.rows_per_gate = (int)(d.rows_per_gate < d.rows ? d.rows_per_gate : d.rows);
   p.C8 = C8;
-  p.crew_rows = (int)(turns * teams);
+  p.crew_rows = (int)(turns * teams * R);
   p.post_layer = d.post == SSCONV_NORM_LAYER;
   p.pre_layer = d.pre == SSCONV_NORM_LAYER;
   p.scale = d.scale;

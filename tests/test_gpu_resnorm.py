@@ -155,6 +155,19 @@ def test_wide_rows(c, post, pre):
     _check(Case(5, c, post=post, pre=pre, seed=c))
 
 
+# (blocks take two rows at a time where there are many)
+@pytest.mark.parametrize("c", [1544, 2048, 3584, 4096])
+@pytest.mark.parametrize("rows,per", [(1201, 0), (1202, 7), (1999, 1), (1201, 600)])
+def test_many_wide_rows(c, rows, per):
+    _check(Case(rows, c, rows_per_gate=per, post=LAYER, pre=RMS, seed=rows + c))
+
+
+@pytest.mark.parametrize("c", [8, 24, 2504])
+@pytest.mark.parametrize("post,pre", [(RMS, LAYER), (LAYER, NONE)])
+def test_sums_over_few_images(c, post, pre):
+    _check(Case(1300, c, rows_per_gate=433, post=post, pre=pre, seed=c))
+
+
 @pytest.mark.parametrize("rows", [1, 2, 3, 31, 33, 257, 3001])
 @pytest.mark.parametrize("c", [8, 40, 136, 776])
 def test_numbers_of_rows(rows, c):
