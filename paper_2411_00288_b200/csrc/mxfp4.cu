@@ -17,9 +17,10 @@ namespace {
 // Quantisation.  The scale's exponent comes from the exponent field E of the block's largest magnitude: floor(log2) = E - 127, so
 // the code (bias 127) is E - 2, at least 0; E = 255 (an infinity or a NaN) gives 255.  Elements are multiplied by the inverse
 // power of two (exact) and rounded once.  A thread block takes the 128 rows x 128 channels of a scale image, four lanes a block of
-// 32 and LANES a row (16; 8 or 4 where rows have no more: 402714 x 8 19 us otherwise), and the image is written whole.  2.53 bytes per element;
-// 401408 x 96 in 22.9 us (4.3 TB/s; a quarter of the lanes have no channels there, and conversions and shuffles take their share),
-// 25088 x 1536 in 20.
+// 32, LANES a row and 32 rows at a time, and the image is written whole.  LANES is 16, 8 or 4 where rows have no more (us with 16 lanes
+// / with blocks of 512 threads all the same / so: 402714 x 8 19 / 8.2 / 6.2, 402714 x 64 - / 14.3 / 12.3).  2.53 bytes per element;
+// 401408 x 96 in 22.6 us (4.3 TB/s; a quarter of the lanes have no channels there, and conversions and shuffles take their share),
+// 25088 x 1536 in 18.5.
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -48,15 +49,13 @@ __device__ __forceinline__ uint32_t e2m1_x8(const uint4& v, uint32_t scale_x2) {
   return out;
 }
 
-constexpr int kMxQuantThreads = 512;
-
 template <int LANES>
-__global__ void __launch_bounds__(kMxQuantThreads, 3) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint4* scales, uint32_t rows, uint32_t chunks,
+__global__ void __launch_bounds__(32 * LANES, 48 / LANES) quantize_mxfp4_kernel(const uint4* x, uint32_t* codes, uint4* scales, uint32_t rows, uint32_t chunks,
                                                              uint32_t blocks, uint32_t C8) {
   __shared__ __align__(16) uint32_t image[128];
   grid_launch_dependents();
   const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
-  constexpr uint32_t kRows = kMxQuantThreads / LANES, kTurns = 128 / kRows;  // rows at a time
+  constexpr uint32_t kRows = 32, kTurns = 128 / kRows;  // rows at a time
   const uint32_t lane = threadIdx.x & (LANES - 1), r0 = threadIdx.x / LANES;
   const uint32_t piece = chunk * 16u + lane;  // of 8 channels
   const uint32_t there = rows - tile * 128u;  // rows from the tile's first on
@@ -97,11 +96,11 @@ __device__ __forceinline__ void e2m1_values_x4(uint32_t codes, uint32_t& low, ui
   high = __byte_perm(lo, hi, 0x7362) | ((codes << 4) & 0x8000u) | ((codes << 16) & 0x80000000u);
 }
 template <int LANES>
-__global__ void __launch_bounds__(kMxQuantThreads) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint32_t rows, uint32_t chunks,
+__global__ void __launch_bounds__(32 * LANES) dequantize_mxfp4_kernel(const uint32_t* codes, const uint8_t* scales, uint4* x, uint32_t rows, uint32_t chunks,
                                                                uint32_t blocks, uint32_t C8) {
   grid_launch_dependents();
   const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
-  constexpr uint32_t kRows = kMxQuantThreads / LANES, kTurns = 128 / kRows;
+  constexpr uint32_t kRows = 32, kTurns = 128 / kRows;
   const uint32_t lane = threadIdx.x & (LANES - 1), r0 = threadIdx.x / LANES;
   const uint32_t piece = chunk * 16u + lane;
   const uint32_t there = rows - tile * 128u;
@@ -648,19 +647,24 @@ int32_t mx_device(int dev, int* pairs) {
 
 }  // namespace
 
+// Lanes of a row.
+static int mx_lanes(const MxGeometry& g) { return g.blocks <= 1 ? 4 : g.blocks <= 2 ? 8 : 16; }
+
 cudaError_t launch_quantize_mxfp4(const void* x, int64_t rows, int C, void* codes, void* scales, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
   count_launch();
-  const auto kernel = g.blocks <= 1 ? quantize_mxfp4_kernel<4> : g.blocks <= 2 ? quantize_mxfp4_kernel<8> : quantize_mxfp4_kernel<16>;
-  return launch_dependent(kernel, (unsigned)(g.row_tiles * g.chunks), kMxQuantThreads, st, (const uint4*)x, (uint32_t*)codes, (uint4*)scales,
+  const int lanes = mx_lanes(g);
+  const auto kernel = lanes == 4 ? quantize_mxfp4_kernel<4> : lanes == 8 ? quantize_mxfp4_kernel<8> : quantize_mxfp4_kernel<16>;
+  return launch_dependent(kernel, (unsigned)(g.row_tiles * g.chunks), 32 * lanes, st, (const uint4*)x, (uint32_t*)codes, (uint4*)scales,
                           (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
 cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int C, void* x, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
   count_launch();
-  const auto kernel = g.blocks <= 1 ? dequantize_mxfp4_kernel<4> : g.blocks <= 2 ? dequantize_mxfp4_kernel<8> : dequantize_mxfp4_kernel<16>;
-  return launch_dependent(kernel, (unsigned)(g.row_tiles * g.chunks), kMxQuantThreads, st, (const uint32_t*)codes, (const uint8_t*)scales,
+  const int lanes = mx_lanes(g);
+  const auto kernel = lanes == 4 ? dequantize_mxfp4_kernel<4> : lanes == 8 ? dequantize_mxfp4_kernel<8> : dequantize_mxfp4_kernel<16>;
+  return launch_dependent(kernel, (unsigned)(g.row_tiles * g.chunks), 32 * lanes, st, (const uint32_t*)codes, (const uint8_t*)scales,
                           (uint4*)x, (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
