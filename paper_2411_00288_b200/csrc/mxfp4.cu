@@ -17,10 +17,9 @@ namespace {
 // Quantisation.  The scale's exponent comes from the exponent field E of the block's largest magnitude: floor(log2) = E - 127, so
 // the code (bias 127) is E - 2, at least 0; E = 255 (an infinity or a NaN) gives 255.  Elements are multiplied by the inverse
 // power of two (exact) and rounded once.  A thread block takes the 128 rows x 128 channels of a scale image, four lanes a block of
-// 32, LANES a row and 32 rows at a time, and the image is written whole.  LANES is 16, 8 or 4 where rows have no more (us with 16 lanes
-// / with blocks of 512 threads all the same / so: 402714 x 8 19 / 8.2 / 6.2, 402714 x 64 - / 14.3 / 12.3).  2.53 bytes per element;
-// 401408 x 96 in 22.6 us (4.3 TB/s; a quarter of the lanes have no channels there, and conversions and shuffles take their share),
-// 25088 x 1536 in 18.5.
+// 32, LANES a row and 32 rows at a time, and the image is written whole.  LANES is 16, or 12, 8 or 4 where rows have no more: us there /
+// back with 16 lanes and so, 401408 x 96 22.6 / 20.4 and 17.1 / 17.1 (5.7 TB/s), 402714 x 64 with 8 of blocks of 512 threads 14.3 / 12.3
+// and 12.3 / 11.0, 402714 x 8 19 / - and 6.2 / 5.7.  2.53 bytes per element; 25088 x 1536 in 18.5 us (5.2 TB/s).
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -56,7 +55,7 @@ __global__ void __launch_bounds__(32 * LANES, 48 / LANES) quantize_mxfp4_kernel(
   grid_launch_dependents();
   const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
   constexpr uint32_t kRows = 32, kTurns = 128 / kRows;  // rows at a time
-  const uint32_t lane = threadIdx.x & (LANES - 1), r0 = threadIdx.x / LANES;
+  const uint32_t lane = threadIdx.x % LANES, r0 = threadIdx.x / LANES;
   const uint32_t piece = chunk * 16u + lane;  // of 8 channels
   const uint32_t there = rows - tile * 128u;  // rows from the tile's first on
   grid_dependency_wait();
@@ -78,10 +77,16 @@ __global__ void __launch_bounds__(32 * LANES, 48 / LANES) quantize_mxfp4_kernel(
     const uint32_t code = e == 255u ? 255u : e < 2u ? 0u : e - 2u;
     const uint32_t inverse = ((254u - min(code, 252u)) << 7) * 0x10001u;
     if (r < there && (piece >> 2) < blocks) codes[(uint64_t)(tile * 128u + r) * (4u * blocks) + piece] = e2m1_x8(v[u], inverse);
-    uint32_t word = code << (8u * (lane >> 2));
-    if (LANES > 4) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
-    if (LANES > 8) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
-    if (lane == 0) image[(r & 31u) * 4u + (r >> 5)] = word;
+    if (LANES == 12) {  // (a row's lanes may be in two warps)
+      uint8_t* bytes = reinterpret_cast<uint8_t*>(image + (r & 31u) * 4u + (r >> 5));
+      if ((lane & 3u) == 0) bytes[lane >> 2] = (uint8_t)code;
+      if (lane == 1) bytes[3] = 0;
+    } else {
+      uint32_t word = code << (8u * (lane >> 2));
+      if (LANES > 4) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
+      if (LANES > 8) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
+      if (lane == 0) image[(r & 31u) * 4u + (r >> 5)] = word;
+    }
   }
   __syncthreads();
   if (threadIdx.x < 32) scales[(uint64_t)blockIdx.x * 32u + threadIdx.x] = reinterpret_cast<const uint4*>(image)[threadIdx.x];
@@ -101,7 +106,7 @@ __global__ void __launch_bounds__(32 * LANES) dequantize_mxfp4_kernel(const uint
   grid_launch_dependents();
   const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
   constexpr uint32_t kRows = 32, kTurns = 128 / kRows;
-  const uint32_t lane = threadIdx.x & (LANES - 1), r0 = threadIdx.x / LANES;
+  const uint32_t lane = threadIdx.x % LANES, r0 = threadIdx.x / LANES;
   const uint32_t piece = chunk * 16u + lane;
   const uint32_t there = rows - tile * 128u;
   grid_dependency_wait();
@@ -648,13 +653,13 @@ int32_t mx_device(int dev, int* pairs) {
 }  // namespace
 
 // Lanes of a row.
-static int mx_lanes(const MxGeometry& g) { return g.blocks <= 1 ? 4 : g.blocks <= 2 ? 8 : 16; }
+static int mx_lanes(const MxGeometry& g) { return g.blocks <= 4 ? 4 * g.blocks : 16; }
 
 cudaError_t launch_quantize_mxfp4(const void* x, int64_t rows, int C, void* codes, void* scales, cudaStream_t st) {
   const MxGeometry g = mx_geometry(rows, C);
   count_launch();
   const int lanes = mx_lanes(g);
-  const auto kernel = lanes == 4 ? quantize_mxfp4_kernel<4> : lanes == 8 ? quantize_mxfp4_kernel<8> : quantize_mxfp4_kernel<16>;
+  const auto kernel = lanes == 4 ? quantize_mxfp4_kernel<4> : lanes == 8 ? quantize_mxfp4_kernel<8> : lanes == 12 ? quantize_mxfp4_kernel<12> : quantize_mxfp4_kernel<16>;
   return launch_dependent(kernel, (unsigned)(g.row_tiles * g.chunks), 32 * lanes, st, (const uint4*)x, (uint32_t*)codes, (uint4*)scales,
                           (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
@@ -663,7 +668,7 @@ cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64
   const MxGeometry g = mx_geometry(rows, C);
   count_launch();
   const int lanes = mx_lanes(g);
-  const auto kernel = lanes == 4 ? dequantize_mxfp4_kernel<4> : lanes == 8 ? dequantize_mxfp4_kernel<8> : dequantize_mxfp4_kernel<16>;
+  const auto kernel = lanes == 4 ? dequantize_mxfp4_kernel<4> : lanes == 8 ? dequantize_mxfp4_kernel<8> : lanes == 12 ? dequantize_mxfp4_kernel<12> : dequantize_mxfp4_kernel<16>;
   return launch_dependent(kernel, (unsigned)(g.row_tiles * g.chunks), 32 * lanes, st, (const uint32_t*)codes, (const uint8_t*)scales,
                           (uint4*)x, (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }

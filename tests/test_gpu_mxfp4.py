@@ -51,6 +51,12 @@ def test_quantised_values(rows, c):
     _check_quantised(x.bfloat16())
 
 
+@pytest.mark.parametrize("rows", [33, 128, 1000])
+@pytest.mark.parametrize("c", [48, 56, 64, 72, 80, 88, 104])
+def test_quantised_rows_of_less_than_an_image(rows, c):
+    _check_quantised((_randn(rows * c, rows, c) * torch.exp(2 * _randn(c, rows, 1))).bfloat16())
+
+
 def test_quantised_shapes_of_more_axes():
     x = _randn(3, 2, 5, 7, 64).bfloat16()
     codes, scales = api.ssconv_quantize_mxfp4(x)
