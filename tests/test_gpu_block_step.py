@@ -160,3 +160,31 @@ def test_a_convnext_shaped_block_in_four_bits(batch, hw, c):
     d = want - want.mean(-1, keepdim=True)
     want = d / torch.sqrt((d * d).mean(-1, keepdim=True) + float(np.float32(1e-6))) * gamma.double() + beta.double()
     assert (n.double() - want).abs().max() <= 2.0 ** -8 * want.abs().max() + 1e-5
+
+
+def test_a_bias_that_was_updated_just_before_its_layer():
+    """AdamW on a 4-bit layer's bias, quantisation of its input and the layer, over and over without waiting: each kernel may start
+    while those before it run, and the outputs are those of calls that wait for each other."""
+    g = torch.Generator(device=DEV).manual_seed(21)
+    rows, cin, cout = 5000, 96, 384
+    desc = api.make_desc(rows, 1, 1, cin, cout, 1, 1, bias=True, gelu=True)
+    xs = [_randn(g, rows, cin).bfloat16() for _ in range(3)]
+    wq = api.ssconv_quantize_mxfp4((_randn(g, cout, cin) / cin ** 0.5).bfloat16())
+    grads = [_randn(g, cout) for _ in range(3)]
+    start = _randn(g, cout)
+
+    def steps(wait):
+        bias, m, v = start.clone(), torch.zeros_like(start), torch.zeros_like(start)
+        out = []
+        for t in range(24):
+            api.ssconv_adamw_multi([bias], [grads[t % 3]], [m], [v], t + 1, lr=0.5)
+            wait()
+            xq = api.ssconv_quantize_mxfp4(xs[t % 3])
+            wait()
+            out.append(api.ssconv_forward_dense_mxfp4(desc, *xq, *wq, bias))
+            wait()
+        return out
+
+    apart = steps(torch.cuda.synchronize)
+    together = steps(lambda: None)
+    assert all(torch.equal(a, b) for a, b in zip(apart, together))
