@@ -18,6 +18,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <memory>
 #include <tuple>
 #include <type_traits>
 #include <utility>
@@ -260,21 +261,22 @@ PyObject* checked(PyObject* const* args, Py_ssize_t n, Py_ssize_t expected) {
   END_HANDLE_TH_ERRORS
 }
 
-// Lists (or tuples) of contiguous fp32 tensors, or bf16 ones where the call takes them, on the current device, as many and of the
-// same extents in each list.
+// Lists (or what else gives tensors one after the other) of contiguous fp32 tensors, or bf16 ones where the call takes them, on the
+// current device, as many and of the same extents in each list.  The tensors are held until the call is made: a generator's are
+// nobody else's, and another thread may change a list.
 struct TensorList {
+  struct Release {
+    void operator()(PyObject* o) const { Py_DECREF(o); }
+  };
+  std::unique_ptr<PyObject, Release> items;
   std::vector<void*> p;
   std::vector<int64_t> n;
   std::vector<int32_t> type;
   at::Tensor first;  // (undefined: an empty list)
   TensorList(PyObject* o, bool takes_bf16, const TensorList* like) {
-    PyObject* items = PySequence_Fast(o, "a list of tensors is expected");
+    items.reset(PySequence_Tuple(o));
     if (items == nullptr) throw PythonError{};
-    struct Release {
-      PyObject* o;
-      ~Release() { Py_DECREF(o); }
-    } release{items};
-    const Py_ssize_t count = PySequence_Fast_GET_SIZE(items);
+    const Py_ssize_t count = PyTuple_GET_SIZE(items.get());
     if (count > INT32_MAX) raise(PyExc_ValueError, "too many tensors");
     if (like != nullptr && (size_t)count != like->n.size()) raise(PyExc_ValueError, "the lists have different lengths");
     p.reserve(count);
@@ -282,7 +284,7 @@ struct TensorList {
     type.reserve(count);
     int device = -1;
     for (Py_ssize_t i = 0; i < count; ++i) {
-      const at::Tensor& t = as_tensor(PySequence_Fast_GET_ITEM(items, i));
+      const at::Tensor& t = as_tensor(PyTuple_GET_ITEM(items.get(), i));
       if (i == 0 && t.is_cuda()) device = c10::cuda::current_device();
       if (!on(device, t)) raise(PyExc_ValueError, "tensors must be contiguous and on the current CUDA device");
       const bool bf16 = t.scalar_type() == at::kBFloat16;

@@ -262,3 +262,19 @@ def test_bounds_at_the_ends():
     assert torch.equal(out[0], g)
     api.ssconv_clip_grads([g], torch.full_like(norm, math.inf), math.inf, out=out)
     assert out[0].isnan().all()
+
+
+def test_tensors_that_only_a_generator_gives():
+    """Nobody but the call holds them: their memory must not be handed out again before it is made."""
+    g = _grads([4096, 100, 70_000], 31)
+    want = api.ssconv_grad_norm(g)
+    for _ in range(10):
+        assert torch.equal(api.ssconv_grad_norm(t.clone() for t in g), want)
+        scaled = api.ssconv_clip_grads((t.clone() for t in g), want, 0.5)
+        assert all(torch.equal(a, b) for a, b in zip(scaled, api.ssconv_clip_grads(g, want, 0.5, out=(torch.empty_like(t) for t in g))))
+        assert len(scaled) == 3
+    theta, m, v = ([torch.zeros_like(t) for t in g] for _ in range(3))
+    one = [[t.clone() for t in s] for s in (theta, m, v)]
+    api.ssconv_adamw_multi(theta, g, m, v, 1, norm=want, max_norm=0.5)
+    api.ssconv_adamw_multi(iter(one[0]), (t.clone() for t in g), iter(one[1]), iter(one[2]), 1, norm=want, max_norm=0.5)
+    assert all(torch.equal(a, b) for s, o in zip((theta, m, v), one) for a, b in zip(s, o))
