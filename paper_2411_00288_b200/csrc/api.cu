@@ -245,8 +245,8 @@ int32_t check_mxfp4(int64_t rows, int32_t C) {
   if (rows < 0 || C <= 0) return SSCONV_ERR_BAD_DESC;
   if (C % 8 != 0 || rows > 0x7FFFFF00LL) return SSCONV_ERR_UNSUPPORTED_SHAPE;
   const ssconv::MxGeometry g = ssconv::mx_geometry(rows, C);
-  // (row, chunk of 128 channels) pairs and pieces of 8 channels are numbered in 32 bits, blocks of 256 pieces in 31
-  if (g.row_tiles * 128 * g.chunks > 0xFFFFFF00LL) return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  // images are numbered in 31 bits: each is a block of a grid, and a row of the map that pairs of blocks copy scales through
+  if (g.row_tiles * g.chunks > 0x7FFFFFFFLL) return SSCONV_ERR_UNSUPPORTED_SHAPE;
   return SSCONV_OK;
 }
 size_t code_bytes_of(const ssconv::MxGeometry& g, int64_t rows) { return (size_t)rows * g.blocks * 16; }

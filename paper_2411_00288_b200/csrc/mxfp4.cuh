@@ -22,7 +22,7 @@ struct MxGeometry {
   int chunks;        // ceil(C/128): images per 128 rows
   int64_t row_tiles; // ceil(rows/128)
 };
-inline MxGeometry mx_geometry(int64_t rows, int C) { return {(C + 31) / 32, (C + 127) / 128, (rows + 127) / 128}; }
+inline MxGeometry mx_geometry(int64_t rows, int64_t C) { return {(int)((C + 31) / 32), (int)((C + 127) / 128), (rows + 127) / 128}; }
 
 cudaError_t launch_quantize_mxfp4(const void* x, int64_t rows, int C, void* codes, void* scales, cudaStream_t st);
 cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int C, void* x, cudaStream_t st);

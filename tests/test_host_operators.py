@@ -304,3 +304,14 @@ def test_adamw_finds_one_overlap_among_many_tensors(order):
             moved[which][i] += step * (4096 - 16) // 4096
             theta, g, m, v = _arrays(*moved)
             assert f(theta, g, m, v, _counts(*[1024 - 4] * count), None, count, 1, 1.0, 0.9, 0.999, 1e-8, 0.0, None, 1.0, None) == BAD
+
+
+def test_mxfp4_sizes_of_the_longest_rows():
+    """ceil(C / 32) and ceil(C / 128) up to the last C of 31 bits."""
+    for c in (2147483520, 2147483528, 2147483608, 2147483616, 2147483640):
+        for rows in (1, 127, 4000):
+            assert api.ssconv_sizes_mxfp4(rows, c) == (rows * -(-c // 32) * 16, -(-rows // 128) * -(-c // 128) * 512)
+    for rows, c in ((128 * 128 + 1, 2147483640), (2147483392, 128 * 129)):  # 2^31 scale images and more
+        with pytest.raises(api.SsconvError) as e:
+            api.ssconv_sizes_mxfp4(rows, c)
+        assert e.value.status == SHAPE
