@@ -354,7 +354,7 @@ PyObject* adamw_multi(PyObject* const* a) {
 int64_t elements(const ssconv_resnorm_t& d) { return d.rows * d.C; }
 // (of a descriptor that the library refuses any number will do: nothing is allocated by it)
 int64_t gates(const ssconv_resnorm_t& d) {
-  return d.rows_per_gate > 0 ? (d.rows + d.rows_per_gate - 1) / d.rows_per_gate * d.C : d.C;
+  return d.rows_per_gate > 0 ? (d.rows / d.rows_per_gate + (d.rows % d.rows_per_gate != 0)) * d.C : d.C;
 }
 
 struct ResNormInputs {

@@ -326,3 +326,16 @@ def test_refusals():
         api.ssconv_residual_norm_backward(case.desc, case.x, case.b, stats, case.dh, None)
     with pytest.raises(api.SsconvError):
         case.backward(stats, ws=torch.empty(64, dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("per", [40, 41, 1 << 31, (1 << 63) - 1])
+def test_one_row_of_gates_for_more_rows_than_there_are(per):
+    one, all_rows = Case(40, 96, rows_per_gate=per), Case(40, 96)
+    assert all(torch.equal(s, t) for s, t in zip((one.x, one.b, one.gate, *one.params), (all_rows.x, all_rows.b, all_rows.gate, *all_rows.params)))
+    for a, b in zip(one.forward(), all_rows.forward()):
+        assert torch.equal(a, b)
+    stats = one.forward()[2]
+    a, b = one.backward(stats), all_rows.backward(stats)
+    assert a.dgate.shape == (1, 96)
+    _check(one)
+    assert torch.equal(a.dx, b.dx) and torch.equal(a.db, b.db)
