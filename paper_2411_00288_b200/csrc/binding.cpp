@@ -303,7 +303,8 @@ struct TensorList {
 // grad_norm(grads, kind, norm, ws) -> (status, norm)
 PyObject* grad_norm(PyObject* const* a) {
   const TensorList g(a[0], true, nullptr);
-  const int32_t kind = (int32_t)as_int(a[1]);
+  const int64_t kind = as_int(a[1]);
+  if (kind != (int32_t)kind) raise(PyExc_ValueError, "kind: GRAD_NORM_L2 or GRAD_NORM_INF is expected");
   expect(a[2], "norm", at::kFloat, 1);
   if (!g.first.defined() && (a[2] == Py_None || a[3] == Py_None))
     raise(PyExc_ValueError, "without gradients the norm's tensor and the scratch have to be given");
@@ -319,7 +320,7 @@ PyObject* grad_norm(PyObject* const* a) {
   }
   void* stream = current_stream();
   return results(without_gil([&] {
-                   return ssconv_grad_norm(g.p.data(), g.n.data(), g.type.data(), g.size(), kind, static_cast<float*>(address(norm)), address(ws),
+                   return ssconv_grad_norm(g.p.data(), g.n.data(), g.type.data(), g.size(), (int32_t)kind, static_cast<float*>(address(norm)), address(ws),
                                            ws.nbytes(), stream);
                  }),
                  norm);

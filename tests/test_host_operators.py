@@ -315,3 +315,8 @@ def test_mxfp4_sizes_of_the_longest_rows():
         with pytest.raises(api.SsconvError) as e:
             api.ssconv_sizes_mxfp4(rows, c)
         assert e.value.status == SHAPE
+
+
+def test_kinds_of_norm_beyond_31_bits_are_refused():
+    with pytest.raises(ValueError, match="kind"):
+        api.ssconv_grad_norm([], kind=1 << 32)
