@@ -849,8 +849,16 @@ def ssconv_dgrad_spread(desc: Desc, dy: torch.Tensor, stream=None) -> torch.Tens
 
 
 # ----------------------------------------------------------------------------- all tensors of a network
-# (These calls and the ones below check and allocate their tensors in the native binding, all for the current stream: another one,
-# a torch stream, is made current around them.)
+# (These calls and the ones below check and allocate their tensors in the native binding, all for the current stream: another one
+# is made current around them.)
+def _on(stream):
+    """The context in which a stream (torch's, or any object with `cuda_stream`) is the current one."""
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream.cuda_stream
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
 GRAD_NORM_L2, GRAD_NORM_INF = 0, 1
 
 
@@ -865,7 +873,7 @@ def ssconv_grad_norm(grads, kind: int = GRAD_NORM_L2, norm: Optional[torch.Tenso
     """fp32 [1] on the device: the root of the sum of all squares (GRAD_NORM_L2), or the largest magnitude (GRAD_NORM_INF), of
     a list of fp32 or bf16 tensors (not synchronised)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream):
             return ssconv_grad_norm(grads, kind, norm, ws)
     rc, norm = _binding().grad_norm(grads, kind, norm, ws)
     _check("ssconv_grad_norm", rc)
@@ -878,7 +886,7 @@ def ssconv_clip_grads(grads, norm: torch.Tensor, max_norm: float, out=None, stre
     grads = grads if isinstance(grads, (list, tuple)) else list(grads)  # (what gives its tensors once is read twice here)
     out = out if out is None or isinstance(out, (list, tuple)) else list(out)
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream):
             return ssconv_clip_grads(grads, norm, max_norm, out)
     if out is None:
         out = grads
@@ -891,7 +899,7 @@ def ssconv_adamw_multi(theta, g, m, v, step: int, lr: float = 1.0, beta1: float 
     """ssconv_adamw of every tensor of the lists theta, m, v (fp32, modified) with the gradients g (fp32 or bf16); with `norm`
     the gradients are scaled as by ssconv_clip_grads on the way (g itself stays as it is)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream):
             return ssconv_adamw_multi(theta, g, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm)
     _check("ssconv_adamw_multi", _binding().adamw_multi(theta, g, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm)[0])
 
@@ -919,7 +927,7 @@ def ssconv_residual_norm(desc: ResNorm, x: torch.Tensor, b: torch.Tensor, gate: 
     """(h, y or None, stats or None): h = scale x + gate post(b), y = pre(h), bf16 like x; stats fp32 [rows, 4] for the backward
     call.  gate fp32 [C] or [ceil(rows / rows_per_gate), C]; gammas and betas fp32 [C], None for ones and zeros."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream):
             return ssconv_residual_norm(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, want_stats, h, y, stats)
     rc, h, y, stats = _binding().residual_norm(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, want_stats, h, y, stats)
     _check("ssconv_residual_norm", rc)
@@ -953,7 +961,7 @@ def ssconv_residual_norm_backward(desc: ResNorm, x: torch.Tensor, b: torch.Tenso
     """Gradients from dh and dy (bf16 like x; dh may be None) and the forward call's inputs and stats: dx, db bf16, the others
     fp32 and of their inputs' shapes, one for each gate, gamma and beta that is given (parts of one allocation)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream):
             return ssconv_residual_norm_backward(desc, x, b, stats, dh, dy, gate, post_gamma, post_beta, pre_gamma, pre_beta, ws)
     rc, *grads = _binding().residual_norm_backward(desc, x, b, gate, post_gamma, post_beta, pre_gamma, pre_beta, stats, dh, dy, ws)
     _check("ssconv_residual_norm_backward", rc)
@@ -972,7 +980,7 @@ def ssconv_quantize_mxfp4(x: torch.Tensor, codes: Optional[torch.Tensor] = None,
     """(codes, scales) uint8 of bf16 x [..., C]: e2m1 elements, one power of two per 32 channels; scales in the tile order that
     ssconv_forward_dense_mxfp4 reads; new ones are parts of one allocation.  Weights [C_out, C_in] are quantised by the same call."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream):
             return ssconv_quantize_mxfp4(x, codes, scales)
     rc, codes, scales = _binding().quantize_mxfp4(x, codes, scales)
     _check("ssconv_quantize_mxfp4", rc)
@@ -982,7 +990,7 @@ def ssconv_quantize_mxfp4(x: torch.Tensor, codes: Optional[torch.Tensor] = None,
 def ssconv_dequantize_mxfp4(codes: torch.Tensor, scales: torch.Tensor, C: int, x: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The bf16 values [..., C] that codes and scales stand for (exact)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream):
             return ssconv_dequantize_mxfp4(codes, scales, C, x)
     rc, x = _binding().dequantize_mxfp4(codes, scales, C, x)
     _check("ssconv_dequantize_mxfp4", rc)
@@ -995,7 +1003,7 @@ def ssconv_forward_dense_mxfp4(desc: Desc, x_codes: torch.Tensor, x_scales: torc
     """Point-wise layer on microscaled 4-bit activations and weights (both from ssconv_quantize_mxfp4); bf16 output
     [N,H,W,C_out] (enqueued, not synchronised)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream):
             return ssconv_forward_dense_mxfp4(desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status)
     rc, y = _binding().forward_dense_mxfp4(desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status)
     _check("ssconv_forward_dense_mxfp4", rc)

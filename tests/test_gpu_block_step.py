@@ -188,3 +188,34 @@ def test_a_bias_that_was_updated_just_before_its_layer():
     apart = steps(torch.cuda.synchronize)
     together = steps(lambda: None)
     assert all(torch.equal(a, b) for a, b in zip(apart, together))
+
+
+@pytest.mark.parametrize("own", [True, False], ids=["a_stream", "the_default_stream"])
+def test_streams_that_are_not_torchs(own):
+    """Any object with `cuda_stream`, as the calls of the convolutions take it."""
+    side = torch.cuda.Stream() if own else torch.cuda.default_stream()
+
+    class Raw:
+        cuda_stream = side.cuda_stream
+
+    def calls(stream):
+        g = torch.Generator(device=DEV).manual_seed(3)
+        grads = [_randn(g, 300), _randn(g, 70)]
+        theta, m, v = ([torch.zeros_like(t) for t in grads] for _ in range(3))
+        x, b, dy = (_randn(g, 40, 96).bfloat16() for _ in range(3))
+        w = _randn(g, 64, 96).bfloat16()
+        torch.cuda.synchronize()
+        norm = api.ssconv_grad_norm(grads, stream=stream)
+        clipped = api.ssconv_clip_grads(grads, norm, 0.5, out=[torch.empty_like(t) for t in grads], stream=stream)
+        api.ssconv_adamw_multi(theta, grads, m, v, 1, norm=norm, max_norm=0.5, stream=stream)
+        d = api.make_resnorm(40, 96)
+        h, y, stats = api.ssconv_residual_norm(d, x, b, want_stats=True, stream=stream)
+        r = api.ssconv_residual_norm_backward(d, x, b, stats, None, dy, stream=stream)
+        xq, wq = api.ssconv_quantize_mxfp4(y, stream=stream), api.ssconv_quantize_mxfp4(w, stream=stream)
+        out = api.ssconv_forward_dense_mxfp4(api.make_desc(40, 1, 1, 96, 64, 1, 1, bias=False), *xq, *wq, stream=stream)
+        back = api.ssconv_dequantize_mxfp4(*xq, 96, stream=stream)
+        assert torch.cuda.current_stream() == torch.cuda.default_stream()
+        torch.cuda.synchronize()
+        return [norm, *clipped, *theta, *m, *v, h, y, stats, r.dx, r.db, out, back]
+
+    assert all(torch.equal(a, b) for a, b in zip(calls(Raw()), calls(None)))
