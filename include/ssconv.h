@@ -572,6 +572,10 @@ int32_t ssconv_dequantize_mxfp4(const void* codes, const void* scales, int64_t r
  * flags as for ssconv_forward; pointers 16-byte aligned. */
 int32_t ssconv_forward_dense_mxfp4(const ssconv_desc_t* desc, const void* x_codes, const void* x_scales, const void* w_codes,
                                    const void* w_scales, const float* bias, void* y, int32_t* dev_status, void* stream);
+/* How that call would run: output channels of a tile (64, 128 or 192), whether tiles of 256 pixels are shared by pairs of thread
+ * blocks, and the number of thread blocks; on the current device (sm_count = 0), or by host arithmetic alone on one of sm_count SMs
+ * that holds `pairs` > 0 pairs at a time.  As ssconv_plan, a tuning aid that launches nothing; any output may be NULL. */
+int32_t ssconv_plan_mxfp4(const ssconv_desc_t* desc, int32_t sm_count, int32_t pairs, int32_t* columns, int32_t* pair, int32_t* ctas);
 
 /* Folding of f neighbouring output pixels of a row into the output channels.  A tile of the forward
  * kernels always spends 128 accumulator rows on output channels, so a layer with C_out <= 64 wastes

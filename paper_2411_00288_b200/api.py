@@ -40,7 +40,8 @@ EXPORTS = ("ssconv_version", "ssconv_launch_count", "ssconv_status_string", "ssc
            "ssconv_forward_fp8", "ssconv_forward_dense_fp8",
            "ssconv_grad_norm_ws_bytes", "ssconv_grad_norm", "ssconv_clip_grads", "ssconv_adamw_multi",
            "ssconv_residual_norm", "ssconv_residual_norm_ws_bytes", "ssconv_residual_norm_backward",
-           "ssconv_sizes_mxfp4", "ssconv_quantize_mxfp4", "ssconv_dequantize_mxfp4", "ssconv_forward_dense_mxfp4")
+           "ssconv_sizes_mxfp4", "ssconv_quantize_mxfp4", "ssconv_dequantize_mxfp4", "ssconv_forward_dense_mxfp4",
+           "ssconv_plan_mxfp4")
 
 
 class SsconvError(RuntimeError):
@@ -144,6 +145,7 @@ def _prototypes():
         "ssconv_quantize_mxfp4": (i32, [vp, i64, i32, vp, vp, vp]),
         "ssconv_dequantize_mxfp4": (i32, [vp, vp, i64, i32, vp, vp]),
         "ssconv_forward_dense_mxfp4": (i32, [vp] * 9),
+        "ssconv_plan_mxfp4": (i32, [vp, i32, i32] + [vp] * 3),
     }
 
 
@@ -1008,3 +1010,12 @@ def ssconv_forward_dense_mxfp4(desc: Desc, x_codes: torch.Tensor, x_scales: torc
     rc, y = _binding().forward_dense_mxfp4(desc, x_codes, x_scales, w_codes, w_scales, bias, y, dev_status)
     _check("ssconv_forward_dense_mxfp4", rc)
     return y
+
+
+def ssconv_plan_mxfp4(desc: Desc, sm_count: int = 0, pairs: int = 0) -> dict:
+    """Output channels of a tile, whether pairs of thread blocks share tiles, and thread blocks of ssconv_forward_dense_mxfp4 on the
+    current device, or on one of `sm_count` SMs that holds `pairs` pairs at a time (host arithmetic only)."""
+    out = [ctypes.c_int32(0) for _ in range(3)]
+    f = lib().ssconv_plan_mxfp4
+    _check("ssconv_plan_mxfp4", f(ctypes.byref(desc), int(sm_count), int(pairs), *[ctypes.byref(o) for o in out]))
+    return dict(columns=out[0].value, pair=bool(out[1].value), ctas=out[2].value)

@@ -249,6 +249,13 @@ int32_t check_mxfp4(int64_t rows, int32_t C) {
   if (g.row_tiles * g.chunks > 0x7FFFFFFFLL) return SSCONV_ERR_UNSUPPORTED_SHAPE;
   return SSCONV_OK;
 }
+int32_t check_pointwise_mxfp4(const ssconv_desc_t* desc) {
+  const int32_t rc = check_desc(desc, true);
+  if (rc != SSCONV_OK) return rc;
+  if (desc->KH != 1 || desc->KW != 1 || desc->stride_h != 1 || desc->stride_w != 1 || desc->pad_h != 0 || desc->pad_w != 0)
+    return SSCONV_ERR_UNSUPPORTED_SHAPE;
+  return check_mxfp4((int64_t)desc->N * desc->H * desc->W, desc->C_in);
+}
 size_t code_bytes_of(const ssconv::MxGeometry& g, int64_t rows) { return (size_t)rows * g.blocks * 16; }
 size_t scale_bytes_of(const ssconv::MxGeometry& g) { return (size_t)g.row_tiles * g.chunks * ssconv::kMxImageBytes; }
 bool apart_mxfp4(const void* x, int64_t rows, int32_t C, const void* codes, const void* scales, bool to_codes) {
@@ -1315,13 +1322,16 @@ int32_t ssconv_dequantize_mxfp4(const void* codes, const void* scales, int64_t r
   return ssconv::launch_dequantize_mxfp4(codes, scales, rows, C, x_bf16, (cudaStream_t)stream) == cudaSuccess ? SSCONV_OK : SSCONV_ERR_CUDA;
 }
 
+int32_t ssconv_plan_mxfp4(const ssconv_desc_t* desc, int32_t sm_count, int32_t pairs, int32_t* columns, int32_t* pair, int32_t* ctas) {
+  const int32_t rc = check_pointwise_mxfp4(desc);
+  if (rc != SSCONV_OK) return rc;
+  if (sm_count < 0 || (sm_count > 0 && pairs <= 0)) return SSCONV_ERR_BAD_DESC;
+  return ssconv::plan_mxfp4(*desc, sm_count, pairs, columns, pair, ctas);
+}
+
 int32_t ssconv_forward_dense_mxfp4(const ssconv_desc_t* desc, const void* x_codes, const void* x_scales, const void* w_codes,
                                    const void* w_scales, const float* bias, void* y, int32_t* dev_status, void* stream) {
-  int32_t rc = check_desc(desc, true);
-  if (rc != SSCONV_OK) return rc;
-  if (desc->KH != 1 || desc->KW != 1 || desc->stride_h != 1 || desc->stride_w != 1 || desc->pad_h != 0 || desc->pad_w != 0)
-    return SSCONV_ERR_UNSUPPORTED_SHAPE;
-  rc = check_mxfp4((int64_t)desc->N * desc->H * desc->W, desc->C_in);
+  const int32_t rc = check_pointwise_mxfp4(desc);
   if (rc != SSCONV_OK) return rc;
   if (!x_codes || !x_scales || !w_codes || !w_scales || !y) return SSCONV_ERR_NULL;
   if ((desc->flags & SSCONV_FLAG_BIAS) && !bias) return SSCONV_ERR_NULL;

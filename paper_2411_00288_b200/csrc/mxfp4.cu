@@ -653,6 +653,38 @@ int32_t mx_device(int dev, int* pairs) {
   return SSCONV_OK;
 }
 
+// The form that a product of this extent takes on a device with so many SMs, which holds so many pairs of blocks at a time.
+struct MxChoice {
+  int columns;
+  bool pair;
+};
+MxChoice mx_choose(const MxGeometry& gx, int C_out, int act, int sms, int pairs) {
+  // The width, by cycles (fitted to 401408 x 96 -> 384 and 8192 x 4096 -> 4096): a tile takes the longer of filling shared memory and
+  // of its epilogue, and the first of the one and the last of the other are not hidden.  Shared memory fills at 50 bytes per cycle and
+  // SM, 12 TB/s out of L2 in all, which is what long K is bound by (with three of four MMAs left out 8192 x 4096 -> 4096 took 62 us, with
+  // all of them 63.7).  Pairs halve the weights' share of it, at a lower rate.  us at 192 / 128 / 64 columns / 192 on pairs: 401408 x 96
+  // -> 384 71.5 / 74.8 / 87.5 / 99.8, 8192 x 4096 -> 4096 69.8 / 76.9 / 126 / 63.7, 25088 x 1536 -> 384 13.3 / 12.7 / 18.8 / 14.4, 1024 x
+  // 4096 -> 4096 17.4 / 14.4 / 21.6 / 16.5, 512 x 1024 -> 1024 7.2 / 6.2 / 5.2 / 7.7.
+  const int mx_stages = (gx.blocks + 7) / 8;
+  MxChoice best = {0, false};
+  double least = 0.0;
+  const auto consider = [&](int w, bool two) {
+    const int64_t rows_of_tiles = two ? (gx.row_tiles + 1) / 2 : gx.row_tiles, at_once = two ? pairs : sms;
+    const int64_t turns = (rows_of_tiles * ((C_out + w - 1) / w) + at_once - 1) / at_once;
+    const double fill = mx_stages * (two ? 790.0 : (128 + w + 8) * 128 / 50.0), epilogue = 800.0 + w * (act == kActGelu ? 19.0 : 14.0);
+    const double cost = turns * (fill > epilogue ? fill : epilogue) + (fill > epilogue ? epilogue : fill);
+    if (best.columns == 0 || cost < (two ? 0.95 : 0.9) * least) {
+      best = {w, two};
+      least = cost;
+    }
+  };
+  consider(192, false);
+  consider(128, false);
+  consider(64, false);
+  consider(192, true);
+  return best;
+}
+
 }  // namespace
 
 // Lanes of a row.
@@ -676,6 +708,23 @@ cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64
                           (uint4*)x, (uint32_t)rows, (uint32_t)g.chunks, (uint32_t)g.blocks, (uint32_t)(C / 8));
 }
 
+int32_t plan_mxfp4(const ssconv_desc_t& d, int sms, int pairs, int32_t* columns, int32_t* pair, int32_t* ctas) {
+  const MxGeometry gx = mx_geometry((int64_t)d.N * d.H * d.W, d.C_in);
+  if (sms == 0) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SSCONV_ERR_CUDA;
+    const int32_t known = mx_device(dev, &pairs);
+    if (known != SSCONV_OK) return known;
+    sms = device_sms();
+  }
+  const MxChoice c = mx_choose(gx, d.C_out, activation_of(d.flags), sms, pairs);
+  const int64_t tiles = (c.pair ? (gx.row_tiles + 1) / 2 : gx.row_tiles) * ((d.C_out + c.columns - 1) / c.columns), at_once = c.pair ? pairs : sms;
+  if (columns) *columns = c.columns;
+  if (pair) *pair = c.pair;
+  if (ctas) *ctas = (int32_t)((tiles < at_once ? tiles : at_once) * (c.pair ? 2 : 1));
+  return SSCONV_OK;
+}
+
 int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales,
                              const float* bias, void* y, int32_t* dev_status, cudaStream_t st) {
   const int64_t rows = (int64_t)d.N * d.H * d.W;
@@ -687,31 +736,9 @@ int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const 
   if (known != SSCONV_OK) return known;
   const int sms = device_sms();
   const int act = activation_of(d.flags);
-  // The width, by cycles (fitted to 401408 x 96 -> 384 and 8192 x 4096 -> 4096): a tile takes the longer of filling shared memory and
-  // of its epilogue, and the first of the one and the last of the other are not hidden.  Shared memory fills at 50 bytes per cycle and
-  // SM, 12 TB/s out of L2 in all, which is what long K is bound by (with three of four MMAs left out 8192 x 4096 -> 4096 took 62 us, with
-  // all of them 63.7).  Pairs halve the weights' share of it, at a lower rate.  us at 192 / 128 / 64 columns / 192 on pairs: 401408 x 96
-  // -> 384 71.5 / 74.8 / 87.5 / 99.8, 8192 x 4096 -> 4096 69.8 / 76.9 / 126 / 63.7, 25088 x 1536 -> 384 13.3 / 12.7 / 18.8 / 14.4, 1024 x
-  // 4096 -> 4096 17.4 / 14.4 / 21.6 / 16.5, 512 x 1024 -> 1024 7.2 / 6.2 / 5.2 / 7.7.
-  const int mx_stages = (gx.blocks + 7) / 8;
-  int bn = 0;
-  bool pair = false;
-  double least = 0.0;
-  const auto consider = [&](int w, bool two) {
-    const int64_t rows_of_tiles = two ? (gx.row_tiles + 1) / 2 : gx.row_tiles, at_once = two ? pairs : sms;
-    const int64_t turns = (rows_of_tiles * ((d.C_out + w - 1) / w) + at_once - 1) / at_once;
-    const double fill = mx_stages * (two ? 790.0 : (128 + w + 8) * 128 / 50.0), epilogue = 800.0 + w * (act == kActGelu ? 19.0 : 14.0);
-    const double cost = turns * (fill > epilogue ? fill : epilogue) + (fill > epilogue ? epilogue : fill);
-    if (bn == 0 || cost < (two ? 0.95 : 0.9) * least) {
-      bn = w;
-      pair = two;
-      least = cost;
-    }
-  };
-  consider(192, false);
-  consider(128, false);
-  consider(64, false);
-  consider(192, true);
+  const MxChoice choice = mx_choose(gx, d.C_out, act, sms, pairs);
+  const int bn = choice.columns;
+  const bool pair = choice.pair;
   int smem = 0;
   const MxKernel kernel = pair        ? mx_kernel<192, true>(act, &smem)
                           : bn == 192 ? mx_kernel<192, false>(act, &smem)

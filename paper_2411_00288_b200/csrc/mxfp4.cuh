@@ -26,6 +26,7 @@ inline MxGeometry mx_geometry(int64_t rows, int64_t C) { return {(int)((C + 31) 
 
 cudaError_t launch_quantize_mxfp4(const void* x, int64_t rows, int C, void* codes, void* scales, cudaStream_t st);
 cudaError_t launch_dequantize_mxfp4(const void* codes, const void* scales, int64_t rows, int C, void* x, cudaStream_t st);
+int32_t plan_mxfp4(const ssconv_desc_t& d, int sms, int pairs, int32_t* columns, int32_t* pair, int32_t* ctas);  // (sms 0: the current device)
 int32_t launch_forward_mxfp4(const ssconv_desc_t& d, const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales,
                              const float* bias, void* y, int32_t* dev_status, cudaStream_t st);
 

@@ -320,3 +320,21 @@ def test_mxfp4_sizes_of_the_longest_rows():
 def test_kinds_of_norm_beyond_31_bits_are_refused():
     with pytest.raises(ValueError, match="kind"):
         api.ssconv_grad_norm([], kind=1 << 32)
+
+
+def test_plan_of_the_4_bit_product():
+    def plan(rows, cin, cout, sms=148, pairs=70, **k):
+        return api.ssconv_plan_mxfp4(api.make_desc(rows, 1, 1, cin, cout, 1, 1, **k), sms, pairs)
+
+    assert plan(1, 2048, 1000) == dict(columns=64, pair=False, ctas=16)
+    assert plan(401408, 96, 384) == dict(columns=192, pair=False, ctas=148)
+    assert plan(6000, 4096, 1536) == dict(columns=192, pair=True, ctas=140)
+    assert plan(401408, 96, 384, sms=100, pairs=50) == dict(columns=192, pair=False, ctas=100)
+    for bad, status in ((dict(sms=-1), BAD), (dict(pairs=0), BAD), (dict(rows=0), BAD), (dict(cin=12), SHAPE), (dict(relu=True, gelu=True), BAD)):
+        with pytest.raises(api.SsconvError) as e:
+            plan(**{**dict(rows=4, cin=64, cout=64), **bad})
+        assert e.value.status == status
+    assert api.lib().ssconv_plan_mxfp4(None, 148, 70, None, None, None) == NULL
+    d = ctypes.byref(api.make_desc(4, 1, 1, 64, 64, 1, 1))
+    assert api.lib().ssconv_plan_mxfp4(d, 148, 70, None, None, None) == 0
+    assert api.lib().ssconv_plan_mxfp4(ctypes.byref(api.make_desc(4, 3, 3, 64, 64, 3, 3, pad=1)), 148, 70, None, None, None) == SHAPE
