@@ -278,3 +278,39 @@ def test_tensors_that_only_a_generator_gives():
     api.ssconv_adamw_multi(theta, g, m, v, 1, norm=want, max_norm=0.5)
     api.ssconv_adamw_multi(iter(one[0]), (t.clone() for t in g), iter(one[1]), iter(one[2]), 1, norm=want, max_norm=0.5)
     assert all(torch.equal(a, b) for s, o in zip((theta, m, v), one) for a, b in zip(s, o))
+
+
+def _chunks(count, tensors, ragged):
+    """Extents of `tensors` tensors that are cut into `count` chunks of 2048; ragged: the last chunk of each has one element."""
+    per = [count // tensors + (i < count % tensors) for i in range(tensors)]
+    return [2048 * k - 2047 * ragged for k in per]
+
+
+# where another form of the norm is taken: 32, 64 and 128 chunks are the warps of one, two and four blocks of a cluster, 256 the last ones
+# that one launch takes, 32 and 384 tensors the most of a kernel's argument; 1184 blocks make a launch of 148 SMs, and from
+# 1184 * 4096 and 1184 * 8192 elements on chunks are longer
+LIMITS = {f"{c}_chunks_of_{t}{'_ragged' if r else ''}": _chunks(c, t, r)
+          for c in (32, 33, 64, 65, 128, 129, 256, 257) for t in (1, 32) for r in (False, True) if c >= t}
+LIMITS.update({f"{t}_tensors": [2049 + i for i in range(t - 1)] + [5] for t in (31, 32, 33, 383, 384, 385, 768, 769)})
+LIMITS.update({f"{t}_tensors_between_empty_ones": [0, 0] + [100 + i for i in range(t)] + [0, 0, 0] for t in (32, 33, 384, 385)})
+LIMITS.update({f"{n}_elements": [n - 3, 3] for n in (1184 * 2048, 1184 * 2048 + 4, 1184 * 4096 - 1, 1184 * 4096, 1184 * 8192 - 1, 1184 * 8192)})
+
+
+@pytest.mark.parametrize("dtypes", [(torch.float32,), (torch.float32, torch.bfloat16)], ids=["f32", "both"])
+@pytest.mark.parametrize("name", LIMITS)
+def test_at_the_limits_of_the_forms(name, dtypes):
+    grads = _grads(LIMITS[name], 3, dtypes)
+    grads[-1].mul_(50)                                          # (the last chunk counts)
+    host = [_f64(g) for g in grads]
+    for kind, inf in ((api.GRAD_NORM_L2, False), (api.GRAD_NORM_INF, True)):
+        want, got = optim.grad_norm(host, inf), float(api.ssconv_grad_norm(grads, kind))
+        assert got == want if inf else abs(got - want) <= 6 * U * want
+    norm = api.ssconv_grad_norm(grads)
+    factor = optim.clip_factor(optim.grad_norm(host), 0.5)
+    for o, g, dtype in zip(api.ssconv_clip_grads(grads, norm, 0.5, out=[torch.full_like(g, 9) for g in grads]), host, (g.dtype for g in grads)):
+        assert (np.abs(_f64(o) - g * factor) <= (9 * U if dtype is torch.float32 else 2.0 ** -8) * np.abs(g * factor) + 2.0 ** -149).all()
+    theta, m, v = ([torch.ones(n, device=DEV) for n in LIMITS[name]] for _ in range(3))
+    before = [tuple(t.clone() for t in s) for s in zip(theta, m, v)]
+    hyper = (1e-2, 0.9, 0.999, 1e-8, 1e-2)
+    api.ssconv_adamw_multi(theta, grads, m, v, 5, *hyper, norm=norm, max_norm=0.5)
+    _check_update(before, list(zip(theta, m, v)), grads, factor, 5, hyper)
