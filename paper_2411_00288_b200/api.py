@@ -885,13 +885,13 @@ def ssconv_grad_norm(grads, kind: int = GRAD_NORM_L2, norm: Optional[torch.Tenso
 def ssconv_clip_grads(grads, norm: torch.Tensor, max_norm: float, out=None, stream=None):
     """Scale every gradient by min(1, max_norm / (norm + 1e-6)), norm as ssconv_grad_norm wrote it: in place, or into the
     tensors of `out` (of the same types); returns the list of results."""
-    grads = grads if isinstance(grads, (list, tuple)) else list(grads)  # (what gives its tensors once is read twice here)
-    out = out if out is None or isinstance(out, (list, tuple)) else list(out)
+    if out is None:
+        out = grads = grads if isinstance(grads, (list, tuple)) else list(grads)  # (what gives its tensors once is read twice)
+    elif not isinstance(out, (list, tuple)):
+        out = list(out)
     if stream is not None:
         with _on(stream):
             return ssconv_clip_grads(grads, norm, max_norm, out)
-    if out is None:
-        out = grads
     _check("ssconv_clip_grads", _binding().clip_grads(grads, out, norm, max_norm)[0])
     return out
 

@@ -18,6 +18,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <memory>
 #include <tuple>
 #include <type_traits>
@@ -263,28 +264,32 @@ PyObject* checked(PyObject* const* args, Py_ssize_t n, Py_ssize_t expected) {
 
 // Lists (or what else gives tensors one after the other) of contiguous fp32 tensors, or bf16 ones where the call takes them, on the
 // current device, as many and of the same extents in each list.  The tensors are held until the call is made: a generator's are
-// nobody else's, and another thread may change a list.
+// nobody else's, and another thread may change a list.  (One piece of memory, of the list itself where it has few tensors.)
 struct TensorList {
-  struct Release {
-    void operator()(PyObject* o) const { Py_DECREF(o); }
-  };
-  std::unique_ptr<PyObject, Release> items;
-  std::vector<void*> p;
-  std::vector<int64_t> n;
-  std::vector<int32_t> type;
+  static constexpr size_t kFew = 32;
+  PyObject** items;  // held
+  void** p;
+  int64_t* n;
+  int32_t* type;
+  int32_t count = 0;
   at::Tensor first;  // (undefined: an empty list)
   TensorList(PyObject* o, bool takes_bf16, const TensorList* like) {
-    items.reset(PySequence_Tuple(o));
-    if (items == nullptr) throw PythonError{};
-    const Py_ssize_t count = PyTuple_GET_SIZE(items.get());
-    if (count > INT32_MAX) raise(PyExc_ValueError, "too many tensors");
-    if (like != nullptr && (size_t)count != like->n.size()) raise(PyExc_ValueError, "the lists have different lengths");
-    p.reserve(count);
-    n.reserve(count);
-    type.reserve(count);
+    const Owned sequence{PySequence_Fast(o, "a list of tensors is expected")};
+    if (sequence.o == nullptr) throw PythonError{};
+    const Py_ssize_t all = PySequence_Fast_GET_SIZE(sequence.o);
+    if (all > INT32_MAX) raise(PyExc_ValueError, "too many tensors");
+    if (like != nullptr && all != like->count) raise(PyExc_ValueError, "the lists have different lengths");
+    const size_t room = (size_t)all <= kFew ? kFew : (size_t)all;
+    if (room > kFew) many.reset(new uint64_t[room * kBytes / 8 + 1]);
+    items = reinterpret_cast<PyObject**>(room > kFew ? many.get() : few);
+    p = reinterpret_cast<void**>(items + room);
+    n = reinterpret_cast<int64_t*>(p + room);
+    type = reinterpret_cast<int32_t*>(n + room);
+    held.list = this;  // (from here on what is held is released, also if a tensor is refused)
     int device = -1;
-    for (Py_ssize_t i = 0; i < count; ++i) {
-      const at::Tensor& t = as_tensor(PyTuple_GET_ITEM(items.get(), i));
+    for (Py_ssize_t i = 0; i < all; ++i) {
+      PyObject* const item = PySequence_Fast_GET_ITEM(sequence.o, i);
+      const at::Tensor& t = as_tensor(item);
       if (i == 0 && t.is_cuda()) device = c10::cuda::current_device();
       if (!on(device, t)) raise(PyExc_ValueError, "tensors must be contiguous and on the current CUDA device");
       const bool bf16 = t.scalar_type() == at::kBFloat16;
@@ -292,12 +297,33 @@ struct TensorList {
       if (bf16 && !takes_bf16) raise(PyExc_TypeError, "float32 tensors are expected");
       if (like != nullptr && t.numel() != like->n[i]) raise(PyExc_ValueError, "tensors of one position have different extents");
       if (i == 0) first = t;
-      p.push_back(address(t));
-      n.push_back(t.numel());
-      type.push_back(bf16 ? SSCONV_BF16 : SSCONV_F32);
+      Py_INCREF(item);
+      items[i] = item;
+      p[i] = address(t);
+      n[i] = t.numel();
+      type[i] = bf16 ? SSCONV_BF16 : SSCONV_F32;
+      ++count;
     }
   }
-  int32_t size() const { return (int32_t)p.size(); }
+  TensorList(const TensorList&) = delete;
+  TensorList& operator=(const TensorList&) = delete;
+  bool same_types(const TensorList& other) const { return std::equal(type, type + count, other.type, other.type + other.count); }
+
+ private:
+  struct Owned {
+    PyObject* o;
+    ~Owned() { Py_XDECREF(o); }
+  };
+  struct Release {
+    TensorList* list = nullptr;
+    ~Release() {
+      for (int32_t i = 0; list != nullptr && i < list->count; ++i) Py_DECREF(list->items[i]);
+    }
+  };
+  static constexpr size_t kBytes = sizeof(PyObject*) + sizeof(void*) + sizeof(int64_t) + sizeof(int32_t);  // of a tensor
+  uint64_t few[kFew * kBytes / 8];
+  std::unique_ptr<uint64_t[]> many;
+  Release held;  // (the last member: it goes first)
 };
 
 // grad_norm(grads, kind, norm, ws) -> (status, norm)
@@ -314,13 +340,13 @@ PyObject* grad_norm(PyObject* const* a) {
     expect(a[3], "ws", ws.scalar_type(), ws.numel());
   } else {
     size_t bytes = 0;
-    const int32_t rc = ssconv_grad_norm_ws_bytes(g.size(), &bytes);
+    const int32_t rc = ssconv_grad_norm_ws_bytes(g.count, &bytes);
     if (rc != SSCONV_OK) return results(rc, at::Tensor());
     ws = given_or_new(Py_None, {(int64_t)bytes}, at::kByte, g.first);
   }
   void* stream = current_stream();
   return results(without_gil([&] {
-                   return ssconv_grad_norm(g.p.data(), g.n.data(), g.type.data(), g.size(), (int32_t)kind, static_cast<float*>(address(norm)), address(ws),
+                   return ssconv_grad_norm(g.p, g.n, g.type, g.count, (int32_t)kind, static_cast<float*>(address(norm)), address(ws),
                                            ws.nbytes(), stream);
                  }),
                  norm);
@@ -329,12 +355,12 @@ PyObject* grad_norm(PyObject* const* a) {
 // clip_grads(grads, out, norm, max_norm) -> (status,)
 PyObject* clip_grads(PyObject* const* a) {
   const TensorList g(a[0], true, nullptr), out(a[1], true, &g);
-  if (g.type != out.type) raise(PyExc_TypeError, "a gradient and its output have different types");
+  if (!g.same_types(out)) raise(PyExc_TypeError, "a gradient and its output have different types");
   const float* norm = static_cast<const float*>(expect(a[2], "norm", at::kFloat, 1));
   const float max_norm = (float)as_double(a[3]);
   void* stream = current_stream();
   return results(without_gil(
-      [&] { return ssconv_clip_grads(g.p.data(), out.p.data(), g.n.data(), g.type.data(), g.size(), norm, max_norm, stream); }));
+      [&] { return ssconv_clip_grads(g.p, out.p, g.n, g.type, g.count, norm, max_norm, stream); }));
 }
 
 // adamw_multi(theta, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm) -> (status,)
@@ -347,7 +373,7 @@ PyObject* adamw_multi(PyObject* const* a) {
   const float max_norm = (float)as_double(a[11]);
   void* stream = current_stream();
   return results(without_gil([&] {
-    return ssconv_adamw_multi(theta.p.data(), g.p.data(), m.p.data(), v.p.data(), g.n.data(), g.type.data(), g.size(), (int32_t)step, lr, beta1,
+    return ssconv_adamw_multi(theta.p, g.p, m.p, v.p, g.n, g.type, g.count, (int32_t)step, lr, beta1,
                               beta2, eps, decay, norm, max_norm, stream);
   }));
 }

@@ -4,6 +4,7 @@ Tolerances, in units of u = 2^-24 (half a step of fp32): the squares of up to 8 
 most, all terms positive, so 9 u relative), their sums in 64 bits; the root halves that and is rounded once: 6 u.  The factor adds
 the rounding of norm + 1e-6 and of the quotient: 8 u; a scaled fp32 gradient one more: 9 u; a bf16 one 2^-8."""
 import math
+import sys
 
 import numpy as np
 import pytest
@@ -314,3 +315,22 @@ def test_at_the_limits_of_the_forms(name, dtypes):
     hyper = (1e-2, 0.9, 0.999, 1e-8, 1e-2)
     api.ssconv_adamw_multi(theta, grads, m, v, 5, *hyper, norm=norm, max_norm=0.5)
     _check_update(before, list(zip(theta, m, v)), grads, factor, 5, hyper)
+
+
+@pytest.mark.parametrize("count", [3, 32, 33, 100])
+def test_calls_hold_no_tensor_afterwards(count):
+    g = _grads([7] * count, 32)
+    norm = api.ssconv_grad_norm(g)
+
+    def references():
+        return [sys.getrefcount(t) for t in g]
+
+    before = references()
+    api.ssconv_grad_norm(g)
+    api.ssconv_clip_grads(g, norm, 0.5, out=[torch.empty_like(t) for t in g])
+    for bad in (torch.zeros(7), torch.zeros(8, device=DEV), torch.zeros(7, device=DEV, dtype=torch.float16), None):
+        with pytest.raises((TypeError, ValueError)):
+            api.ssconv_clip_grads(g, norm, 0.5, out=g[:-1] + [bad])
+    with pytest.raises(ValueError):
+        api.ssconv_clip_grads(g, norm, 0.5, out=g[:-1])
+    assert references() == before
