@@ -496,8 +496,9 @@ int32_t ssconv_forward_dense_fp8(const ssconv_desc_t* desc, const void* x_e4m3, 
  * at a time and does not clip.
  *
  * ssconv_grad_norm:  norm[0] = sqrt(sum of all squares) (SSCONV_GRAD_NORM_L2) or the largest magnitude (SSCONV_GRAD_NORM_INF); 0
- *   without elements.  Sums are held in 64 bits and taken in an order that depends on the counts alone, so that results are
- *   reproducible; no finite gradients overflow on the way.  A NaN among the gradients makes the norm NaN (an infinity makes it
+ *   without elements.  Squares are added eight at a time in 32 bits where nothing is lost by it (tensors that start at a 16-byte
+ *   boundary; one by one in 64 bits otherwise), those sums in 64 bits, in an order that depends on the counts, on which tensors are
+ *   aligned so and on the device's number of SMs: the same call gives the same bits; no finite gradients overflow on the way.  A NaN among the gradients makes the norm NaN (an infinity makes it
  *   infinite).  norm: device fp32 [1]; ws: device scratch of ssconv_grad_norm_ws_bytes(tensors) bytes, 8-byte aligned, that no
  *   other call in flight uses.
  * ssconv_clip_grads:  out[i] = g[i] * min(1, max_norm / (norm + 1e-6)), in the type of g[i], rounded once; norm as written by
@@ -525,8 +526,8 @@ int32_t ssconv_adamw_multi(void* const* theta, const void* const* g, void* const
  * or SSCONV_NORM_RMS (v / sqrt(mean(v^2) + eps) * gamma + beta).  gamma, beta: fp32 [C], NULL for ones and zeros.  gate: fp32,
  * NULL (ones), [C] with rows_per_gate = 0, or [ceil(rows / rows_per_gate)][C]: row r takes gates r / rows_per_gate.  x, b, h, y: bf16
  * [rows][C]; arithmetic in fp32, y is the norm of h before h is rounded.  stats (nullable): fp32 [rows][4], what the backward call
- * needs of both norms (mean and 1/deviation of b, then of h).  h (nullable if y is wanted) and y may be the buffer of x or of b;
- * any other overlap of what is written is SSCONV_ERR_BAD_DESC.
+ * needs of both norms (mean and 1/deviation of b, then of h).  h (nullable if y is wanted) and y may be the buffer of x or of b
+ * (which the backward call, if there is one, has to be given as they were); any other overlap of what is written is SSCONV_ERR_BAD_DESC.
  * C % 8 == 0, C <= 8192, rows <= 2^30 (rows = 0 is a no-op); tensors 16-byte aligned. */
 enum { SSCONV_NORM_NONE = 0, SSCONV_NORM_LAYER = 1, SSCONV_NORM_RMS = 2 };
 typedef struct {

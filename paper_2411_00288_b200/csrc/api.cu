@@ -1,5 +1,6 @@
 // extern "C" boundary: argument validation and dispatch to the launchers.  Nothing here
-// touches device memory, synchronises or allocates.
+// synchronises or allocates device memory, and device memory is touched in one place: the gradients of residual norms without
+// rows are cleared.
 #include <cuda_runtime.h>
 
 #include <algorithm>

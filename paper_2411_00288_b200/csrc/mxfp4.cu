@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(MxTile<BN, PAIR>::kThreads, 1) mxfp4_kernel(co
             split2(v, lo, hi);
             w[j] = activate_pack<ACT>(lo, hi);
           }
-          if (i == 0) {  // (not before: 401408 x 96 -> 384 93.8 us instead of 97.3, 12544 x 2048 -> 512 11.7 instead of 12.3)
+          if (i == 0) {  // (not before: it took 401408 x 96 -> 384 from 97.3 us to 93.8, 12544 x 2048 -> 512 from 12.3 to 11.7)
             if (lane == 0) bulk_wait_group_read0();  // the warp's last piece has left its buffer
             __syncwarp();
           }
@@ -661,10 +661,12 @@ struct MxChoice {
 MxChoice mx_choose(const MxGeometry& gx, int C_out, int act, int sms, int pairs) {
   // The width, by cycles (fitted to 401408 x 96 -> 384 and 8192 x 4096 -> 4096): a tile takes the longer of filling shared memory and
   // of its epilogue, and the first of the one and the last of the other are not hidden.  Shared memory fills at 50 bytes per cycle and
-  // SM, 12 TB/s out of L2 in all, which is what long K is bound by (with three of four MMAs left out 8192 x 4096 -> 4096 took 62 us, with
-  // all of them 63.7).  Pairs halve the weights' share of it, at a lower rate.  us at 192 / 128 / 64 columns / 192 on pairs: 401408 x 96
-  // -> 384 71.5 / 74.8 / 87.5 / 99.8, 8192 x 4096 -> 4096 69.8 / 76.9 / 126 / 63.7, 25088 x 1536 -> 384 13.3 / 12.7 / 18.8 / 14.4, 1024 x
-  // 4096 -> 4096 17.4 / 14.4 / 21.6 / 16.5, 512 x 1024 -> 1024 7.2 / 6.2 / 5.2 / 7.7.
+  // SM, 12 TB/s out of L2 in all, which is most of what long K takes (with three of four MMAs left out 8192 x 4096 -> 4096 took 62.5 us
+  // at 192 columns and 58.1 on pairs, with all of them 69.8 and 63.6).  Pairs halve the weights' share of it, at a lower rate.  us at 192 /
+  // 128 / 64 columns / 192 on pairs: 401408 x 96 -> 384 76.4 / 78.8 / 90.3 / 101, with GELU 90.7 / 99.6 / 112 / 123, 8192 x 4096 -> 4096 69.8 /
+  // 76.0 / 125 / 63.6, 25088 x 1536 -> 384 13.6 / 13.0 / 18.7 / 14.3, 25088 x 384 -> 1536 with GELU 27.2 / 28.0 / 36.5 / 36.8, 1024 x 4096 ->
+  // 4096 16.6 / 14.4 / 20.5 / 15.8, 512 x 1024 -> 1024 6.1 / 5.5 / 4.8 / 6.9.  (The rule takes the fastest but for 25088 x 1536 -> 384, whose 192
+  // columns come out within the margin of 128 and are 0.6 us slower.)
   const int mx_stages = (gx.blocks + 7) / 8;
   MxChoice best = {0, false};
   double least = 0.0;
