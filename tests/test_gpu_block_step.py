@@ -1,5 +1,10 @@
 """The calls around the convolutions together: a training step of two residual blocks, a mask-learning step that ends in one update
 of all layers' choice weights, and a ConvNeXt-shaped block in 4 bits."""
+import os
+import subprocess
+import sys
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -219,3 +224,75 @@ def test_streams_that_are_not_torchs(own):
         return [norm, *clipped, *theta, *m, *v, h, y, stats, r.dx, r.db, out, back]
 
     assert all(torch.equal(a, b) for a, b in zip(calls(Raw()), calls(None)))
+
+
+def _all_calls(g, i):
+    """Every call once, on extents that differ with i; what each wrote."""
+    grads = [_randn(g, n) for n in (300_000 + i, 5, 77)]
+    theta, m, v = ([torch.zeros_like(t) for t in grads] for _ in range(3))
+    rows, c = 700, (96, 768, 1000, 2048, 5000, 384)[i % 6]
+    x, b, dh, dy = (_randn(g, rows, c).bfloat16() for _ in range(4))
+    gate, w = _randn(g, 7, c), _randn(g, 264, c).bfloat16()
+
+    def run():
+        norm = api.ssconv_grad_norm(grads)
+        clipped = api.ssconv_clip_grads(grads, norm, 0.5, out=[torch.empty_like(t) for t in grads])
+        api.ssconv_adamw_multi(theta, grads, m, v, 1, norm=norm, max_norm=0.5)
+        d = api.make_resnorm(rows, c, rows_per_gate=100, post=1 + i % 2, pre=1 + i // 2 % 2)
+        h, y, stats = api.ssconv_residual_norm(d, x, b, gate=gate, want_stats=True)
+        r = api.ssconv_residual_norm_backward(d, x, b, stats, dh, dy, gate=gate)
+        xq, wq = api.ssconv_quantize_mxfp4(y), api.ssconv_quantize_mxfp4(w)
+        out = api.ssconv_forward_dense_mxfp4(api.make_desc(rows, 1, 1, c, 264, 1, 1, bias=False), *xq, *wq)
+        return [norm, *clipped, *theta, h, y, stats, r.dx, r.db, r.dgate, *xq, out, api.ssconv_dequantize_mxfp4(*xq, c)]
+
+    return run, (theta, m, v)
+
+
+def test_calls_of_four_threads_at_once():
+    streams = [torch.cuda.Stream() for _ in range(4)]
+
+    def work(k, out):
+        with torch.cuda.stream(streams[k]):
+            g = torch.Generator(device=DEV).manual_seed(100 + k)
+            for i in range(24):
+                out.append([t.clone() for t in _all_calls(g, i)[0]()])
+            streams[k].synchronize()
+
+    def all_of(at_once):
+        outs = [[] for _ in streams]
+        threads = [threading.Thread(target=work, args=(k, outs[k])) for k in range(4)]
+        for t in threads:
+            t.start()
+            if not at_once:
+                t.join()
+        for t in threads:
+            t.join()
+        return outs
+
+    together, apart = all_of(True), all_of(False)
+    for a, b in zip(together, apart):
+        assert len(a) == len(b) == 24
+        assert all(torch.equal(s, t) for x, y in zip(a, b) for s, t in zip(x, y))
+
+
+def test_a_process_whose_first_calls_are_recorded():
+    """Nothing that the calls set up once per process is closed to a recording."""
+    code = """
+import torch
+from tests.test_gpu_block_step import DEV, _all_calls
+run, state = _all_calls(torch.Generator(device=DEV).manual_seed(1), 0)
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    out = run()
+graph.replay()
+torch.cuda.synchronize()
+kept = [t.clone() for t in out]
+for tensors in state:
+    for t in tensors:
+        t.zero_()
+assert all(torch.equal(a, b) for a, b in zip(kept, run()))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
