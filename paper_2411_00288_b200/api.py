@@ -855,7 +855,7 @@ def ssconv_dgrad_spread(desc: Desc, dy: torch.Tensor, stream=None) -> torch.Tens
 # is made current around them.)
 def _on(stream):
     """The context in which a stream (torch's, or any object with `cuda_stream`) is the current one."""
-    if not isinstance(stream, torch.cuda.Stream):
+    if not isinstance(stream, torch.Stream):
         handle = stream.cuda_stream
         stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
     return torch.cuda.stream(stream)

@@ -224,6 +224,7 @@ def test_streams_that_are_not_torchs(own):
         return [norm, *clipped, *theta, *m, *v, h, y, stats, r.dx, r.db, out, back]
 
     assert all(torch.equal(a, b) for a, b in zip(calls(Raw()), calls(None)))
+    assert all(torch.equal(a, b) for a, b in zip(calls(torch.Stream(device=DEV)), calls(None)))
 
 
 def _all_calls(g, i):
